@@ -268,6 +268,142 @@ int nt_output_slots(const int64_t *h_offsets, int64_t N, int64_t *total);
 int nt_plan_batches(const int32_t *h_lengths, int64_t N, int64_t budget, int32_t max_rows, int64_t *order,
                     int64_t *batch_starts, int64_t *n_batches);
 
+/*
+ * Paged key/value caches, apart from any model: for callers that decode with layers of their own, and what a model
+ * loaded with self_cache decodes with.
+ *
+ * A cache holds the keys and values of up to max_seqs sequences (ids 0 .. max_seqs - 1, all empty at first) in n_layers
+ * layers.  Memory is handed out in pages of page_tokens tokens; a page holds the same tokens of every layer and head.  A
+ * sequence reaches its pages through a table on the device, so sequences can share pages: a page that several sequences
+ * hold is full, and nothing writes to it.
+ *   kind      NT_CACHE_F16, NT_CACHE_BF16: values are rounded to that type when written (to nearest even).
+ *             NT_CACHE_Q4: 4 bits a value.  Each 32 consecutive values of a head's vector share a scale, the smallest
+ *             number with 3 significant bits, exponent -14 .. 13 and at most 10240 that is at least a sixth of the
+ *             largest magnitude; a value becomes a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times the scale, the nearest,
+ *             halves to the even code; beyond 61440, and for infinities, the largest of its sign.  A block with a NaN
+ *             is NaN as a whole.
+ *   n_q_heads, n_kv_heads, d_head
+ *             query head h reads the keys and values of head h / (n_q_heads / n_kv_heads); d_head 64, 128, 256 or 512
+ *   page_tokens   32, 64, 128 or 256
+ *   n_pages       at most 2^24
+ *   max_len       longest sequence, at most 2^24
+ *
+ * The calls below only enqueue kernels on hip_stream, allocate nothing and may be captured into a graph.  Calls on one
+ * cache must follow one another: in one stream, or ordered by events.  All have to be made with the device current on
+ * which the cache was created.  What the host cannot see is checked on the device: a sequence id outside [0, max_seqs),
+ * the second of two equal ids in a call that changes sequences, a length that does not fit.  Such an entry is skipped, its
+ * sequence stays as it was, and nt_cache_check reports it; so it is where no free pages are left (entries are served in
+ * order; from the first that does not fit on, those that need pages are skipped).  The lowest free pages are
+ * handed out first, so page tables do not depend on timing.
+ *
+ * d_seq [n] int32 names the sequences of a call, NULL = 0 .. n - 1; n = 0 is allowed and does nothing.
+ * d_first [n + 1] int32 gives each sequence's rows in the arrays of the call (rows d_first[i] .. d_first[i + 1] - 1 are its
+ * new tokens, in order), NULL = one row each.
+ */
+typedef enum { NT_F32 = 0, NT_F16 = 1, NT_BF16 = 2 } nt_type;
+typedef enum { NT_CACHE_F16 = 1, NT_CACHE_BF16 = 2, NT_CACHE_Q4 = 3 } nt_cache_kind;
+
+typedef struct nt_cache nt_cache; /* opaque */
+
+typedef struct {
+  uint32_t struct_size; /* sizeof(nt_cache_config), checked */
+  int32_t kind, n_layers, n_q_heads, n_kv_heads, d_head;
+  int32_t page_tokens, n_pages, max_seqs, max_len;
+} nt_cache_config;
+
+/* Device memory nt_cache_create takes for this configuration (0 if invalid). */
+int64_t nt_cache_bytes(const nt_cache_config *cfg);
+
+/* Synchronises hip_stream.  Errors: NT_EINVAL, NT_ESHAPE, NT_ENOMEM, NT_EHIP. */
+int nt_cache_create(const nt_cache_config *cfg, void *hip_stream, nt_cache **out);
+
+void nt_cache_destroy(nt_cache *c);
+
+/*
+ * Room for new tokens at the end of sequences: as many as they have rows in d_first, or one each.  Lengths grow at once;
+ * the contents are undefined until nt_cache_write, or nt_cache_attend with k and v, has filled them in every layer.
+ * Errors of this and the following calls: NT_EINVAL (null argument, negative n, type or stride), NT_ESHAPE (n beyond
+ * max_seqs), NT_ERANGE (layer), NT_EHIP.
+ */
+int nt_cache_reserve(nt_cache *c, int32_t n, const int32_t *d_seq, const int32_t *d_first, void *hip_stream);
+
+/*
+ * Fill the tokens that the last nt_cache_reserve gave these sequences (same n, d_seq and d_first as there) in one layer.
+ *   d_k, d_v   [rows, n_kv_heads, d_head] of `type`, ld elements from row to row
+ *   max_new    no sequence has more rows than this in the call (a sequence that has is skipped and reported)
+ */
+int nt_cache_write(nt_cache *c, int32_t layer, int32_t n, const int32_t *d_seq, const int32_t *d_first, int32_t max_new, const void *d_k,
+                   const void *d_v, int64_t ld, int32_t type, void *hip_stream);
+
+/*
+ * Attention of the newest tokens of sequences over the cache, in one layer.  Sequence i has m = d_first[i + 1] - d_first[i]
+ * query rows (one with d_first NULL), at its last m positions.  The query at position p sees key j if
+ *     j <= p, and window == 0 or p - j < window or j < sinks,
+ * so with a window the first `sinks` tokens stay visible.  Keys whose pages have been freed (nt_cache_trim) are not
+ * seen.  out = sum_j w_j v_j / sum_j w_j with w_j = exp(scale * q . k_j) over the seen keys, zeros where none is seen.
+ *   q, out     [rows, n_q_heads, d_head] of `type`, ld_q / ld_out elements from row to row
+ *   k, v       NULL, or the rows' keys and values, which are written to the cache first as by nt_cache_write
+ *   max_new    no sequence has more query rows (a sequence that has more, or more than its length, gets zeros in the
+ *              rows that are too many and is reported)
+ *   max_keys   the longest of the sequences, as far as the caller knows; chooses how the work is split, nothing else.
+ *              0 = max_len
+ * Keys and values that a query does not see have no influence on it, whatever they are.  Scores, weights and sums are
+ * fp32; with one row per sequence the queries and weights enter the products with about twice the bits of the
+ * cache's type (fp16 for 4 bits), with more they are rounded to that type.
+ * Errors as above; NT_EINVAL for a wrong struct_size, a negative window or number of sinks, or only one of k and v.
+ */
+typedef struct {
+  uint32_t struct_size; /* sizeof(nt_attend_args), checked */
+  int32_t layer, n, max_new, max_keys, type, window, sinks;
+  float scale;
+  const int32_t *d_seq, *d_first;
+  const void *q, *k, *v;
+  void *out;
+  int64_t ld_q, ld_kv, ld_out;
+} nt_attend_args;
+int nt_cache_attend(nt_cache *c, const nt_attend_args *a, void *hip_stream);
+
+/*
+ * What one layer holds, in token order: d_k, d_v [n, max_keys, n_kv_heads, d_head] of `type`, dense; zeros behind a
+ * sequence's end and where its pages have been freed.
+ */
+int nt_cache_read(nt_cache *c, int32_t layer, int32_t n, const int32_t *d_seq, int32_t max_keys, void *d_k, void *d_v, int32_t type,
+                  void *hip_stream);
+
+/*
+ * Sequence d_dst[i] becomes what d_src[i] was before the call, for all i at once (a permutation of the hypotheses of a beam is
+ * one call); what it held before is freed.  nt_cache_fork shares the full pages and copies the last, unfilled one;
+ * nt_cache_copy copies every page.  d_src may name a sequence several times.  While the call runs it needs the pages of
+ * the copies on top of those in use.
+ */
+int nt_cache_fork(nt_cache *c, int32_t n, const int32_t *d_src, const int32_t *d_dst, void *hip_stream);
+int nt_cache_copy(nt_cache *c, int32_t n, const int32_t *d_src, const int32_t *d_dst, void *hip_stream);
+
+/*
+ * Cut sequences back to their first d_len[i] tokens (NULL = none: the sequences end) and free the pages that nobody holds any
+ * more.  A page that is shared and cut inside is copied first.  Skipped and reported: a length that is negative, beyond
+ * the sequence, or inside a page that nt_cache_trim has freed.
+ */
+int nt_cache_truncate(nt_cache *c, int32_t n, const int32_t *d_seq, const int32_t *d_len, void *hip_stream);
+
+/*
+ * Free the pages of sequences that neither the newest token nor any later one sees through this window (> 0) with these
+ * sinks.  Positions stay as they are.
+ */
+int nt_cache_trim(nt_cache *c, int32_t n, const int32_t *d_seq, int32_t window, int32_t sinks, void *hip_stream);
+
+/* Move the pages in use to the front of the pool, the last ones into the holes. */
+int nt_cache_compact(nt_cache *c, void *hip_stream);
+
+/* d_len [max_seqs] int32 (optional): lengths; d_pages [2] int32 (optional): pages in use, and the last one in use plus one. */
+int nt_cache_lengths(nt_cache *c, int32_t *d_len, int32_t *d_pages, void *hip_stream);
+
+/*
+ * Read and clear what the device has reported since the last call (synchronises the stream): NT_OK, NT_ERANGE (an entry
+ * was skipped for its id or length) or NT_ENOMEM (for want of pages; both: NT_ENOMEM).
+ */
+int nt_cache_check(nt_cache *c, void *hip_stream);
+
 /* ---- not on the hot path: needed to check parity -------------------------------------- */
 
 /*

@@ -19,7 +19,10 @@ EXPORTS = ["nt_param_count", "nt_n_steps", "nt_load_weights", "nt_free", "nt_enc
            "nt_debug_timing_count", "nt_debug_timing_name", "nt_debug_timing_read", "nt_pipeline_lanes",
            "nt_pipeline_lane", "nt_lane_stream", "nt_decode_greedy_eos", "nt_translate_batch_eos",
            "nt_debug_q8_output_layer", "nt_debug_q8_quantize_row", "nt_output_slots", "nt_debug_set_vocab_tiled",
-           "nt_debug_set_cert_distrust", "nt_q8_output_layer_static", "nt_debug_set_encoder_tails", "nt_debug_probe_peaks"]
+           "nt_debug_set_cert_distrust", "nt_q8_output_layer_static", "nt_debug_set_encoder_tails", "nt_debug_probe_peaks",
+           "nt_cache_bytes", "nt_cache_create", "nt_cache_destroy", "nt_cache_reserve", "nt_cache_write", "nt_cache_attend",
+           "nt_cache_read", "nt_cache_fork", "nt_cache_copy", "nt_cache_truncate", "nt_cache_trim", "nt_cache_compact",
+           "nt_cache_lengths", "nt_cache_check"]
 
 
 class NtConfig(C.Structure):
@@ -28,6 +31,17 @@ class NtConfig(C.Structure):
         "pad_id")] + [("ln_eps", C.c_float), ("max_batch_rows", C.c_int32), ("max_batch_tokens", C.c_int64),
                                 ("pipeline_lanes", C.c_int32), ("dec_n_heads", C.c_int32),
                                 ("dec_d_ffn", C.c_int32), ("ln_l1", C.c_int32), ("q8_output", C.c_int32)]
+
+
+class NtCacheConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(k, C.c_int32) for k in (
+        "kind", "n_layers", "n_q_heads", "n_kv_heads", "d_head", "page_tokens", "n_pages", "max_seqs", "max_len")]
+
+
+class NtAttendArgs(C.Structure):
+    _fields_ = ([("struct_size", C.c_uint32)] + [(k, C.c_int32) for k in ("layer", "n", "max_new", "max_keys", "type", "window", "sinks")] +
+                [("scale", C.c_float)] + [(k, C.c_void_p) for k in ("d_seq", "d_first", "q", "k", "v", "out")] +
+                [(k, C.c_int64) for k in ("ld_q", "ld_kv", "ld_out")])
 
 
 class NtError(RuntimeError):
@@ -84,6 +98,20 @@ def load_library() -> C.CDLL:
         "nt_debug_timing_name": (C.c_char_p, [C.c_int]),
         "nt_debug_timing_read": (C.c_int, [p, C.c_int, C.POINTER(C.c_double), C.POINTER(i64), C.POINTER(C.c_double),
                                            C.POINTER(C.c_double), p]),
+        "nt_cache_bytes": (i64, [C.POINTER(NtCacheConfig)]),
+        "nt_cache_create": (C.c_int, [C.POINTER(NtCacheConfig), p, C.POINTER(p)]),
+        "nt_cache_destroy": (None, [p]),
+        "nt_cache_reserve": (C.c_int, [p, i32, p, p, p]),
+        "nt_cache_write": (C.c_int, [p, i32, i32, p, p, i32, p, p, i64, i32, p]),
+        "nt_cache_attend": (C.c_int, [p, C.POINTER(NtAttendArgs), p]),
+        "nt_cache_read": (C.c_int, [p, i32, i32, p, i32, p, p, i32, p]),
+        "nt_cache_fork": (C.c_int, [p, i32, p, p, p]),
+        "nt_cache_copy": (C.c_int, [p, i32, p, p, p]),
+        "nt_cache_truncate": (C.c_int, [p, i32, p, p, p]),
+        "nt_cache_trim": (C.c_int, [p, i32, p, i32, i32, p]),
+        "nt_cache_compact": (C.c_int, [p, p]),
+        "nt_cache_lengths": (C.c_int, [p, p, p, p]),
+        "nt_cache_check": (C.c_int, [p, p]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -337,3 +365,142 @@ class Model:
                                             int(eos_id), out.ctypes.data_as(C.c_void_p), oo.ctypes.data_as(C.c_void_p),
                                             ol.ctypes.data_as(C.c_void_p), _stream_ptr(stream)))
         return out[:total], oo, ol[:N]
+
+
+CACHE_KINDS = {"f16": 1, "bf16": 2, "q4": 3}
+
+
+class Cache:
+    """Owns one nt_cache: keys and values of many sequences in pages, as fp16, bf16 or 4 bits (kind "f16", "bf16", "q4").
+
+    Methods mirror the C entry points.  Values are cuda tensors of float32, float16 or bfloat16; seqs, first, lengths are contiguous
+    int32 cuda tensors.  seqs None = sequences 0 .. n - 1; first None = one row each."""
+
+    def __init__(self, kind: str, n_layers: int, n_q_heads: int, n_kv_heads: int, d_head: int, n_pages: int, max_seqs: int, max_len: int,
+                 page_tokens: int = 64, stream=None):
+        self.config = self._make_config(kind, n_layers, n_q_heads, n_kv_heads, d_head, n_pages, max_seqs, max_len, page_tokens)
+        h = C.c_void_p()
+        _check(lib().nt_cache_create(C.byref(self.config), _stream_ptr(stream), C.byref(h)))
+        self._h = h
+
+    @staticmethod
+    def _make_config(kind, n_layers, n_q_heads, n_kv_heads, d_head, n_pages, max_seqs, max_len, page_tokens=64) -> NtCacheConfig:
+        return NtCacheConfig(C.sizeof(NtCacheConfig), CACHE_KINDS[kind], n_layers, n_q_heads, n_kv_heads, d_head, page_tokens, n_pages, max_seqs,
+                             max_len)
+
+    @classmethod
+    def bytes(cls, *args, **kw) -> int:
+        """Device memory that a cache with these arguments takes (0 if they are invalid)."""
+        c = cls._make_config(*args, **kw)
+        return int(lib().nt_cache_bytes(C.byref(c)))
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().nt_cache_destroy(self._h)
+        self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _type(self, *tensors) -> int:
+        import torch
+        types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+        if any(t.dtype is not tensors[0].dtype for t in tensors) or tensors[0].dtype not in types:
+            raise TypeError("tensors of one type, float32, float16 or bfloat16, are needed")
+        return types[tensors[0].dtype]
+
+    @staticmethod
+    def _ints(t, size):
+        import torch
+        if t is None:
+            return None
+        if t.dtype is not torch.int32 or not t.is_cuda or not t.is_contiguous() or t.numel() < size:
+            raise TypeError(f"a contiguous int32 cuda tensor of at least {size} entries is needed")
+        return t.data_ptr()
+
+    def _rows(self, t, heads):
+        """Row stride of a [rows, heads, d_head] tensor whose heads are dense."""
+        d = self.config.d_head
+        if not t.is_cuda or t.dim() != 3 or tuple(t.shape[1:]) != (heads, d) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+            raise TypeError(f"a cuda tensor [rows, {heads}, {d}] with dense heads is needed")
+        return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * d)
+
+    def _count(self, n, seqs):
+        if n is None and seqs is None:
+            raise TypeError("n or seqs is needed")
+        return seqs.numel() if n is None else int(n)
+
+    def reserve(self, n: int = None, seqs=None, first=None, stream=None):
+        n = self._count(n, seqs)
+        _check(lib().nt_cache_reserve(self._h, n, self._ints(seqs, n), self._ints(first, n + 1), _stream_ptr(stream)))
+
+    def write(self, k, v, n: int = None, seqs=None, first=None, max_new: int = 1, layer: int = 0, stream=None):
+        n, heads = self._count(n, seqs), self.config.n_kv_heads
+        ld = self._rows(k, heads)
+        if self._rows(v, heads) != ld or k.shape != v.shape:
+            raise TypeError("k and v need the same shape and strides")
+        if first is None and k.shape[0] < n:
+            raise TypeError(f"{n} rows are needed")
+        _check(lib().nt_cache_write(self._h, layer, n, self._ints(seqs, n), self._ints(first, n + 1), max_new, k.data_ptr(), v.data_ptr(), ld,
+                                    self._type(k, v), _stream_ptr(stream)))
+
+    def attend(self, q, out, n: int = None, seqs=None, first=None, k=None, v=None, max_new: int = 1, max_keys: int = 0, window: int = 0,
+               sinks: int = 0, scale: float = None, layer: int = 0, stream=None):
+        n, g = self._count(n, seqs), self.config
+        a = NtAttendArgs(C.sizeof(NtAttendArgs), layer, n, max_new, max_keys, 0, window, sinks, g.d_head ** -0.5 if scale is None else scale)
+        a.d_seq, a.d_first = self._ints(seqs, n), self._ints(first, n + 1)
+        a.q, a.out, a.ld_q, a.ld_out = q.data_ptr(), out.data_ptr(), self._rows(q, g.n_q_heads), self._rows(out, g.n_q_heads)
+        tensors = [q, out]
+        if out.shape != q.shape:
+            raise TypeError("q and out need the same shape")
+        if k is not None or v is not None:
+            if k is None or v is None or k.shape != v.shape or k.shape[0] != q.shape[0] or self._rows(k, g.n_kv_heads) != self._rows(v, g.n_kv_heads):
+                raise TypeError("k and v need q's rows, and the same shape and strides")
+            a.k, a.v, a.ld_kv = k.data_ptr(), v.data_ptr(), self._rows(k, g.n_kv_heads)
+            tensors += [k, v]
+        if first is None and q.shape[0] < n:
+            raise TypeError(f"{n} rows are needed")
+        a.type = self._type(*tensors)
+        _check(lib().nt_cache_attend(self._h, C.byref(a), _stream_ptr(stream)))
+
+    def read(self, k, v, n: int = None, seqs=None, layer: int = 0, stream=None):
+        """k, v [n, max_keys, n_kv_heads, d_head], dense."""
+        n, g = self._count(n, seqs), self.config
+        if k.shape != v.shape or k.dim() != 4 or k.shape[0] < n or tuple(k.shape[2:]) != (g.n_kv_heads, g.d_head) or not (
+                k.is_cuda and v.is_cuda and k.is_contiguous() and v.is_contiguous()):
+            raise TypeError(f"contiguous cuda tensors [{n}, max_keys, {g.n_kv_heads}, {g.d_head}] are needed")
+        _check(lib().nt_cache_read(self._h, layer, n, self._ints(seqs, n), k.shape[1], k.data_ptr(), v.data_ptr(), self._type(k, v),
+                                   _stream_ptr(stream)))
+
+    def fork(self, src, dst, stream=None):
+        n = src.numel()
+        _check(lib().nt_cache_fork(self._h, n, self._ints(src, n), self._ints(dst, n), _stream_ptr(stream)))
+
+    def copy(self, src, dst, stream=None):
+        n = src.numel()
+        _check(lib().nt_cache_copy(self._h, n, self._ints(src, n), self._ints(dst, n), _stream_ptr(stream)))
+
+    def truncate(self, n: int = None, seqs=None, lengths=None, stream=None):
+        """Cut sequences back to these lengths; None ends them."""
+        n = self._count(n, seqs)
+        _check(lib().nt_cache_truncate(self._h, n, self._ints(seqs, n), self._ints(lengths, n), _stream_ptr(stream)))
+
+    def trim(self, window: int, sinks: int = 0, n: int = None, seqs=None, stream=None):
+        n = self._count(n, seqs)
+        _check(lib().nt_cache_trim(self._h, n, self._ints(seqs, n), window, sinks, _stream_ptr(stream)))
+
+    def compact(self, stream=None):
+        _check(lib().nt_cache_compact(self._h, _stream_ptr(stream)))
+
+    def lengths(self, stream=None):
+        """(lengths int32 [max_seqs], pages int32 [2]: in use, and the last one in use plus one), cuda tensors."""
+        import torch
+        n, p = (torch.empty(k, dtype=torch.int32, device="cuda") for k in (self.config.max_seqs, 2))
+        _check(lib().nt_cache_lengths(self._h, n.data_ptr(), p.data_ptr(), _stream_ptr(stream)))
+        return n, p
+
+    def check(self, stream=None):
+        _check(lib().nt_cache_check(self._h, _stream_ptr(stream)))

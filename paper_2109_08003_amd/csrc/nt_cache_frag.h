@@ -1,0 +1,153 @@
+// A tile of a paged cache (nt_cache.h) in the registers of a wave: loads, the rounding of 4-bit codes, the products.
+#pragma once
+#include "nt_cache.h"
+#include "nt_kernels.h"
+
+namespace nt {
+
+template <int KIND> struct FragType { typedef f16x8 type; typedef _Float16 elem; };
+template <> struct FragType<CACHE_BF16> { typedef bf16x8 type; typedef __bf16 elem; };
+
+__device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+// eight codes as fp16 numbers (exact)
+__device__ __forceinline__ void q4_unpack(uint32_t w, f16x2 (&x)[4]) {
+  x[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 0);
+  x[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 1);
+  x[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 2);
+  x[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 3);
+}
+__device__ __forceinline__ f16x8 q4_join(const f16x2 (&x)[4]) {
+  f16x8 r;
+#pragma unroll
+  for (int j = 0; j < 8; j++) r[j] = x[j / 2][j % 2];
+  return r;
+}
+// two scale bytes (at bit positions 16 p and 16 p + 8 of w) as fp16 numbers
+__device__ __forceinline__ f16x2 q4_scale_pair(uint32_t w, int p) {
+  return __builtin_bit_cast(f16x2, p == 0 ? (w & 0xFF) << 8 | (w & 0xFF00) << 16 : (w >> 8 & 0xFF00) | (w & 0xFF000000u));
+}
+
+// Keys of a tile: fragment (t, c) for the first product
+template <int KIND, int DH>
+struct KeyTile {
+  static constexpr int NC = DH / 32;
+  uint4 x[KIND == CACHE_Q4 ? DH / 64 : 2 * NC];
+  uint32_t sc[KIND == CACHE_Q4 ? 2 : 1][KIND == CACHE_Q4 ? (NC + 3) / 4 : 1];
+  __device__ __forceinline__ void load(const char *tile, int lane) {
+    const uint4 *p = (const uint4 *)tile + lane;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(x) / 16); i++) x[i] = p[i * 64];
+    if constexpr (KIND == CACHE_Q4) {
+      const int r = lane & 15, tok = 8 * (r >> 2) + (r & 3);
+#pragma unroll
+      for (int t = 0; t < 2; t++) {
+        const char *s = tile + 32 * DH + (tok + 4 * t) * NC;
+        if constexpr (NC == 2) sc[t][0] = *(const unsigned short *)s;
+        else
+#pragma unroll
+          for (int i = 0; i < NC / 4; i++) sc[t][i] = ((const uint32_t *)s)[i];
+      }
+    }
+  }
+  __device__ __forceinline__ typename FragType<KIND>::type frag(int t, int c) const {
+    if constexpr (KIND != CACHE_Q4) {
+      return __builtin_bit_cast(typename FragType<KIND>::type, x[t * NC + c]);
+    } else {
+      const int w = t * NC + c;
+      f16x2 v[4];
+      q4_unpack(((const uint32_t *)&x[w / 4])[w % 4], v);
+      const uint32_t b = sc[t][c / 4] >> (8 * (c % 4)) & 0xFF;
+      const f16x2 s = __builtin_bit_cast(f16x2, b << 8 | b << 24);
+#pragma unroll
+      for (int j = 0; j < 4; j++) v[j] *= s;
+      return q4_join(v);
+    }
+  }
+};
+
+// Values of a tile: fragment n for the second product
+template <int KIND, int DH>
+struct ValueTile {
+  static constexpr int NV = DH / 16;
+  uint4 x[KIND == CACHE_Q4 ? NV / 4 : NV];
+  uint2 sc[KIND == CACHE_Q4 ? NV / 2 : 1];
+  __device__ __forceinline__ void load(const char *tile, int lane) {
+    const uint4 *p = (const uint4 *)(tile + (KIND == CACHE_Q4 ? 16 : 64) * DH) + lane;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(x) / 16); i++) x[i] = p[i * 64];
+    if constexpr (KIND == CACHE_Q4) {
+#pragma unroll
+      for (int b = 0; b < NV / 2; b++) sc[b] = *(const uint2 *)(tile + 33 * DH + b * kTile + (lane >> 4) * 8);
+    }
+  }
+  // Values of this lane's eight tokens that are no query's become zero, whatever they are: bit j of `keep` stays
+  __device__ __forceinline__ void clear(uint32_t keep) {
+    uint32_t m[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) m[j] = (keep >> (2 * j) & 1 ? 0xFFFFu : 0) | (keep >> (2 * j + 1) & 1 ? 0xFFFF0000u : 0);
+    if constexpr (KIND != CACHE_Q4) {
+#pragma unroll
+      for (int i = 0; i < NV; i++) x[i].x &= m[0], x[i].y &= m[1], x[i].z &= m[2], x[i].w &= m[3];
+    } else {  // a zero scale
+      const uint32_t lo = (m[0] & 0xFF) | (m[0] >> 8 & 0xFF00) | (m[1] << 16 & 0xFF0000) | (m[1] & 0xFF000000u);
+      const uint32_t hi = (m[2] & 0xFF) | (m[2] >> 8 & 0xFF00) | (m[3] << 16 & 0xFF0000) | (m[3] & 0xFF000000u);
+#pragma unroll
+      for (int b = 0; b < NV / 2; b++) sc[b].x &= lo, sc[b].y &= hi;
+    }
+  }
+  __device__ __forceinline__ typename FragType<KIND>::type frag(int n) const {
+    if constexpr (KIND != CACHE_Q4) {
+      return __builtin_bit_cast(typename FragType<KIND>::type, x[n]);
+    } else {
+      f16x2 v[4];
+      q4_unpack(((const uint32_t *)&x[n / 4])[n % 4], v);
+      v[0] *= q4_scale_pair(sc[n / 2].x, 0);
+      v[1] *= q4_scale_pair(sc[n / 2].x, 1);
+      v[2] *= q4_scale_pair(sc[n / 2].y, 0);
+      v[3] *= q4_scale_pair(sc[n / 2].y, 1);
+      return q4_join(v);
+    }
+  }
+};
+
+// exponent bits all set
+__device__ __forceinline__ bool no_number(_Float16 x) { return (__builtin_bit_cast(unsigned short, x) & 0x7C00) == 0x7C00; }
+__device__ __forceinline__ bool no_number(__bf16 x) { return (__builtin_bit_cast(unsigned short, x) & 0x7F80) == 0x7F80; }
+template <class F>
+__device__ __forceinline__ bool any_no_number(F v) {
+  bool b = false;
+#pragma unroll
+  for (int j = 0; j < 8; j++) b |= no_number(v[j]);
+  return b;
+}
+// o += V^T P where some values are infinities or NaN, and some queries do not see all keys: bit j of `seen` says whether
+// this lane's query sees its token j.  Infinities and NaN count for the queries that see them only, the rest is the product.
+template <class F>
+__device__ f32x4 mma_seen(F v, F p, uint32_t seen, f32x4 o) {
+  F fin = v, up = v, down = v, nan = v, see = v;
+#pragma unroll
+  for (int j = 0; j < 8; j++) {
+    const float x = (float)v[j];
+    const bool bad = no_number(v[j]);
+    if (bad) fin[j] = 0;
+    up[j] = bad && x > 0.f ? 1 : 0;
+    down[j] = bad && x < 0.f ? 1 : 0;
+    nan[j] = x != x ? 1 : 0;
+    see[j] = seen >> j & 1 ? 1 : 0;
+  }
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  o = mma(fin, p, o);
+  const f32x4 u = mma(up, see, zero), d = mma(down, see, zero), q = mma(nan, see, zero);
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    if (u[i] > 0.f) o[i] += __builtin_inff();
+    if (d[i] > 0.f) o[i] -= __builtin_inff();
+    if (q[i] > 0.f) o[i] = __builtin_nanf("");
+  }
+  return o;
+}
+
+}  // namespace nt

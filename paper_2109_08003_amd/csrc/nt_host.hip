@@ -47,6 +47,13 @@ int fail(int code, const char *fmt, ...) {
   return code;
 }
 
+}  // namespace
+int nt::set_error(int code, const char *message) {
+  g_err = message;
+  return code;
+}
+namespace {
+
 #define HIP_TRY(expr)                                                                      \
   do {                                                                                     \
     hipError_t _e = (expr);                                                                \

@@ -8,6 +8,10 @@
 
 namespace nt {
 
+// the message of nt_last_error; returns code
+int set_error(int code, const char *message);
+
+
 // ---- GEMM: C[M,N] = A[M,K] * Wt[N,K]^T, fp16 MFMA with fp32 accumulation -------------
 // Epilogue, applied to acc (fp32):  v = acc + bias[n];  if (n < scale_cols) v *= scale;
 // if (relu) v = max(v,0);  if (resid) v += resid[m*ldr+n];  then columns [0,n_split) go to

@@ -1,0 +1,104 @@
+"""Host side of the paged caches on a HIP runtime that runs nothing: what is refused, with which code, and that a refused call launches
+nothing; sizes; which kernels the calls launch."""
+import pytest
+from test_host_launches import host  # noqa: F401  (a fixture)
+
+CACHE = """
+from paper_2109_08003_amd.binding import NtCacheConfig, NtAttendArgs, lib
+L = lib()
+
+def config(kind=1, n_layers=2, n_q_heads=4, n_kv_heads=2, d_head=64, page_tokens=64, n_pages=8, max_seqs=4, max_len=200):
+    return NtCacheConfig(C.sizeof(NtCacheConfig), kind, n_layers, n_q_heads, n_kv_heads, d_head, page_tokens, n_pages, max_seqs, max_len)
+
+def create(**kw):
+    h = C.c_void_p(1)
+    return L.nt_cache_create(C.byref(config(**kw)), None, C.byref(h)), h
+
+x = np.zeros(1 << 16, dtype=np.float32).ctypes.data   # stands for any device buffer
+def attend(h, **kw):
+    a = NtAttendArgs(C.sizeof(NtAttendArgs), 0, 2, 1, 0, 0, 0, 0, 1.0)
+    a.q = a.out = x
+    a.ld_q = a.ld_out = 256
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return L.nt_cache_attend(h, C.byref(a), None)
+"""
+
+
+def test_configurations(host):  # noqa: F811
+    bad, good, null = host(CACHE + """
+bad = [(kw, create(**kw)[0], create(**kw)[1].value, int(L.nt_cache_bytes(C.byref(config(**kw))))) for kw in (
+    dict(kind=0), dict(kind=4), dict(n_layers=0), dict(n_q_heads=3), dict(n_q_heads=1), dict(n_kv_heads=0), dict(d_head=96), dict(d_head=1024),
+    dict(page_tokens=16), dict(page_tokens=48), dict(page_tokens=512), dict(n_pages=0), dict(n_pages=1 << 25), dict(max_seqs=0), dict(max_seqs=65536),
+    dict(max_len=0), dict(max_len=1 << 25), dict(n_pages=1 << 24, page_tokens=256, n_layers=1024, n_kv_heads=4))]
+good = [(k, d, p, create(kind=k, d_head=d, page_tokens=p)[0], int(L.nt_cache_bytes(C.byref(config(kind=k, d_head=d, page_tokens=p)))))
+        for k in (1, 2, 3) for d in (64, 128, 256, 512) for p in (32, 64, 128, 256)]
+c = config(); c.struct_size = 8
+h = C.c_void_p()
+null = [L.nt_cache_create(None, None, C.byref(h)), L.nt_cache_create(C.byref(config()), None, None), L.nt_cache_create(C.byref(c), None, C.byref(h)),
+        L.nt_cache_reserve(None, 1, None, None, None), L.nt_cache_attend(None, None, None), L.nt_cache_compact(None, None), L.nt_cache_check(None, None),
+        int(L.nt_cache_bytes(None))]
+L.nt_cache_destroy(None)
+print(json.dumps((bad, good, null)))
+""")
+    for kw, rc, handle, size in bad:
+        assert rc == (-1 if "kind" in kw else -2) and handle is None and size == 0, kw
+    for kind, width, page, rc, size in good:
+        token = 2 * 2 * (width * 2 if kind < 3 else width // 2 + width // 32)   # two heads, keys and values
+        pool = 2 * 8 * page * token                                            # two layers of eight pages
+        split = 1024 * 8 * (width + 2) * 4
+        assert rc == 0 and pool + split <= size <= pool + split + 32768, (kind, width, page, size - pool - split)
+    assert null == [-1, -1, -1, -1, -1, -1, -1, 0]
+
+
+def test_refusals_launch_nothing(host):  # noqa: F811
+    rcs, launched, empty, launched_empty = host(CACHE + """
+_, h = create()
+stub.stub_clear()
+rcs = {
+  "negative n": L.nt_cache_reserve(h, -1, None, None, None),
+  "too many": L.nt_cache_reserve(h, 5, None, None, None),
+  "layer": L.nt_cache_write(h, 2, 1, None, None, 1, x, x, 128, 0, None),
+  "negative layer": L.nt_cache_write(h, -1, 1, None, None, 1, x, x, 128, 0, None),
+  "type": L.nt_cache_write(h, 0, 1, None, None, 1, x, x, 128, 3, None),
+  "stride": L.nt_cache_write(h, 0, 1, None, None, 1, x, x, 127, 0, None),
+  "max_new": L.nt_cache_write(h, 0, 1, None, None, 201, x, x, 128, 0, None),
+  "no keys": L.nt_cache_write(h, 0, 1, None, None, 1, None, x, 128, 0, None),
+  "struct_size": attend(h, struct_size=7),
+  "window": attend(h, window=-1), "sinks": attend(h, sinks=-1), "max_keys": attend(h, max_keys=-1),
+  "q stride": attend(h, ld_q=255), "out stride": attend(h, ld_out=255), "kv stride": attend(h, k=x, v=x, ld_kv=127),
+  "k alone": attend(h, k=x, ld_kv=128), "no q": attend(h, q=None), "no out": attend(h, out=None),
+  "rows without d_first": attend(h, max_new=2), "attend layer": attend(h, layer=2), "attend type": attend(h, type=9), "attend n": attend(h, n=5),
+  "read": L.nt_cache_read(h, 0, 1, None, 5, None, x, 0, None), "read max_keys": L.nt_cache_read(h, 0, 1, None, -1, x, x, 0, None),
+  "fork": L.nt_cache_fork(h, 1, None, x, None), "copy": L.nt_cache_copy(h, 1, x, None, None),
+  "trim window": L.nt_cache_trim(h, 1, None, 0, 0, None), "trim sinks": L.nt_cache_trim(h, 1, None, 1, -1, None),
+}
+launched = stub.stub_n_launches()
+empty = [L.nt_cache_reserve(h, 0, None, None, None), L.nt_cache_write(h, 0, 0, None, None, 1, None, None, 0, 0, None), attend(h, n=0, q=None, out=None),
+         attend(h, max_new=0, d_first=x), L.nt_cache_read(h, 0, 0, None, 5, None, None, 0, None), L.nt_cache_fork(h, 0, None, None, None),
+         L.nt_cache_truncate(h, 0, None, None, None), L.nt_cache_trim(h, 0, None, 1, 0, None)]
+print(json.dumps((rcs, launched, empty, stub.stub_n_launches())))
+""")
+    want = {"too many": -2, "attend n": -2, "layer": -6, "negative layer": -6, "max_new": -6, "attend layer": -6, "read max_keys": -6}
+    assert {k: v for k, v in rcs.items() if v != want.get(k, -1)} == {}
+    assert launched == 0 and empty == [0] * 8 and launched_empty == 0
+
+
+@pytest.mark.parametrize("kind", [1, 2, 3])
+def test_grids(host, kind):  # noqa: F811
+    """No grid is empty or beyond what the kernels index, from one token to a million."""
+    out = host(CACHE + f"""
+_, h = create(kind={kind}, n_pages=1 << 14, max_len=1 << 20, max_seqs=4)
+out = []
+for n, new, keys in ((1, 1, 1), (4, 1, 0), (1, 1, 1 << 20), (4, 5000, 0), (2, 1 << 20, 0), (3, 2, 100)):
+    stub.stub_clear()
+    rc = attend(h, n=n, max_new=new, max_keys=keys, d_first=x if new > 1 else None, k=x, v=x, ld_kv=128)
+    out.append((n, new, rc, launches()))
+print(json.dumps(out))
+""")
+    for n, new, rc, launches in out:
+        assert rc == 0
+        for name, blocks in launches:
+            assert 0 < blocks < 2 ** 31, (name, blocks)
+        write = [b for name, b in launches if "cache_write" in name]
+        assert write == [((new + 30) // 32 + 1) * 2 * n]
