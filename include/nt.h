@@ -81,6 +81,11 @@ typedef struct nt_model nt_model; /* opaque */
  *                  127 - (mean + 7 sd) / scale and 255 - max / scale.  The logit is
  *                  a_scale * (b_scale[v] * float(I)) with I = sum_k (u_k - a_zero)(q_vk - zero_v) exact.
  *                  Needs d_model 256 or 512.  0: fp16 matrix cores with ~22-bit activations.
+ *   self_cache     0: the decoder's self-attention reads caches of the library's own form, about 22 bits a value; NT_CACHE_F16,
+ *                  NT_CACHE_BF16 or NT_CACHE_Q4 (below): a paged cache of that kind, pages of 32 tokens.  Not with rpr_clip > 0.
+ *   self_window, self_sinks
+ *                  with a paged cache: a target token sees the last self_window tokens, itself among them, and the
+ *                  first self_sinks; self_window 0 = all
  *   max_batch_tokens, max_batch_rows
  *                  largest padded batch (rows x longest row) and most rows per batch the
  *                  arena must hold; the peak footprint is fixed at load time, in the spirit
@@ -99,6 +104,7 @@ typedef struct {
   int32_t dec_n_heads, dec_d_ffn;
   int32_t ln_l1;
   int32_t q8_output;
+  int32_t self_cache, self_window, self_sinks; /* a struct_size that ends before these three is accepted: they are 0 */
 } nt_config;
 
 /* Number of fp16 elements the weight blob of this configuration must hold (0 if invalid). */
@@ -286,6 +292,7 @@ int nt_plan_batches(const int32_t *h_lengths, int64_t N, int64_t budget, int32_t
  *             query head h reads the keys and values of head h / (n_q_heads / n_kv_heads); d_head 64, 128, 256 or 512
  *   page_tokens   32, 64, 128 or 256
  *   n_pages       at most 2^24
+ *   max_seqs      at most 2^20
  *   max_len       longest sequence, at most 2^24
  *
  * The calls below only enqueue kernels on hip_stream, allocate nothing and may be captured into a graph.  Calls on one
@@ -323,7 +330,7 @@ void nt_cache_destroy(nt_cache *c);
  * Room for new tokens at the end of sequences: as many as they have rows in d_first, or one each.  Lengths grow at once;
  * the contents are undefined until nt_cache_write, or nt_cache_attend with k and v, has filled them in every layer.
  * Errors of this and the following calls: NT_EINVAL (null argument, negative n, type or stride), NT_ESHAPE (n beyond
- * max_seqs), NT_ERANGE (layer), NT_EHIP.
+ * max_seqs, or more than 2^31 workgroups), NT_ERANGE (layer), NT_EHIP.
  */
 int nt_cache_reserve(nt_cache *c, int32_t n, const int32_t *d_seq, const int32_t *d_first, void *hip_stream);
 

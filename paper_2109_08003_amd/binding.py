@@ -30,7 +30,11 @@ class NtConfig(C.Structure):
         "n_enc", "n_dec", "d_model", "n_heads", "d_ffn", "vocab", "max_len", "rpr_clip", "tie_output", "bos_id",
         "pad_id")] + [("ln_eps", C.c_float), ("max_batch_rows", C.c_int32), ("max_batch_tokens", C.c_int64),
                                 ("pipeline_lanes", C.c_int32), ("dec_n_heads", C.c_int32),
-                                ("dec_d_ffn", C.c_int32), ("ln_l1", C.c_int32), ("q8_output", C.c_int32)]
+                                ("dec_d_ffn", C.c_int32), ("ln_l1", C.c_int32), ("q8_output", C.c_int32),
+                                ("self_cache", C.c_int32), ("self_window", C.c_int32), ("self_sinks", C.c_int32)]
+
+
+CACHE_KINDS = {"f16": 1, "bf16": 2, "q4": 3}   # nt_cache_kind; in a model's configuration: self_cache
 
 
 class NtCacheConfig(C.Structure):
@@ -143,6 +147,8 @@ def make_config(cfg: dict, max_batch_tokens: int, max_batch_rows: int = 0, pipel
     c.dec_d_ffn = int(cfg.get("dec_d_ffn", 0))
     c.ln_l1 = int(cfg.get("ln_l1", 0))
     c.q8_output = int(cfg.get("q8_output", 0))
+    c.self_cache = CACHE_KINDS.get(cfg.get("self_cache", 0), cfg.get("self_cache", 0))
+    c.self_window, c.self_sinks = int(cfg.get("self_window", 0)), int(cfg.get("self_sinks", 0))
     return c
 
 
@@ -365,9 +371,6 @@ class Model:
                                             int(eos_id), out.ctypes.data_as(C.c_void_p), oo.ctypes.data_as(C.c_void_p),
                                             ol.ctypes.data_as(C.c_void_p), _stream_ptr(stream)))
         return out[:total], oo, ol[:N]
-
-
-CACHE_KINDS = {"f16": 1, "bf16": 2, "q4": 3}
 
 
 class Cache:

@@ -53,7 +53,7 @@ struct CacheRows {
 struct CacheWriteArgs {
   CacheView c;
   CacheRows r;
-  int32_t layer, type;
+  int32_t layer, type, tiles;  // tiles: of a sequence's new tokens, at most
   const void *k, *v;
   long ld;
   int32_t vec;  // rows are 16-byte aligned
@@ -63,7 +63,7 @@ hipError_t launch_cache_write(const CacheWriteArgs &a, hipStream_t s);
 struct CacheReadArgs {
   CacheView c;
   CacheRows r;
-  int32_t layer, type, max_keys;
+  int32_t layer, type, max_keys, tiles;
   void *k, *v;
 };
 hipError_t launch_cache_read(const CacheReadArgs &a, hipStream_t s);
@@ -78,14 +78,14 @@ struct CacheAttnArgs {
   float scale;
   int32_t window, sinks;
   int32_t vec;     // query rows are 16-byte aligned
-  int32_t splits;  // workgroups that share a sequence's keys
+  int32_t row_tiles, splits;  // tiles of 8 query rows of a sequence, workgroups that share their keys
   float *part;     // [workgroup][8 queries][dh + 2]
   int32_t *count;  // [workgroup / splits], zero between calls
 };
 constexpr int kSplitBlocks = 1024;  // workgroups among which split keys are spread, at most
 constexpr int kMaxSplits = 64;      // of one row: the last workgroup reads what the others left
 // Queries in tiles of 8 (rows: token, then head of the group), each split over the keys.  Any number of rows.
-hipError_t launch_cache_token(const CacheAttnArgs &a, int row_tiles, hipStream_t s);
+hipError_t launch_cache_token(const CacheAttnArgs &a, hipStream_t s);
 
 #ifdef __HIPCC__
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));

@@ -480,17 +480,18 @@ template <int KIND>
 __global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteArgs a) {
   extern __shared__ uint32_t lds[];
   const CacheView &c = a.c;
-  const int i = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, dh = c.dh, per = dh / 8;
+  const int x = blockIdx.x % a.tiles, h = blockIdx.x / a.tiles % c.heads, i = blockIdx.x / a.tiles / c.heads;
+  const int tid = threadIdx.x, dh = c.dh, per = dh / 8;
   const int s = a.r.seq ? a.r.seq[i] : i;
   const long row0 = a.r.first ? a.r.first[i] : i;
   const int rows = a.r.first ? a.r.first[i + 1] - (int)row0 : 1;
   const bool known = s >= 0 && s < c.max_seqs;
   const int base = known ? c.base[s] : 0, len = known ? c.len[s] : 0;
   if (!known || rows < 0 || rows > a.r.max_new || c.slot[s] != i || rows != len - base) {
-    if (tid == 0 && blockIdx.x == 0 && h == 0) atomicOr(c.flags, 1);
+    if (tid == 0 && x == 0 && h == 0) atomicOr(c.flags, 1);
     return;
   }
-  const int tile = (base >> 5) + blockIdx.x;
+  const int tile = (base >> 5) + x;
   if (tile * kTile >= len) return;
   const int t0 = max(base - tile * kTile, 0), t1 = min(len - tile * kTile, kTile);
   const int page = c.table[(long)s * c.width + (tile >> (c.page_shift - 5))];
@@ -569,7 +570,8 @@ template <int KIND>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadArgs a) {
   extern __shared__ uint32_t lds[];
   const CacheView &c = a.c;
-  const int i = blockIdx.z, h = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x, dh = c.dh, per = dh / 8;
+  const int tile = blockIdx.x % a.tiles, h = blockIdx.x / a.tiles % c.heads, i = blockIdx.x / a.tiles / c.heads;
+  const int tid = threadIdx.x, dh = c.dh, per = dh / 8;
   const int s = a.r.seq ? a.r.seq[i] : i;
   const bool known = s >= 0 && s < c.max_seqs;
   if (!known && tid == 0 && tile == 0 && h == 0) atomicOr(c.flags, 1);
@@ -626,7 +628,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadArgs a) {
 }  // namespace
 
 hipError_t launch_cache_write(const CacheWriteArgs &a, hipStream_t s) {
-  const dim3 grid((a.r.max_new + kTile - 2) / kTile + 1, a.c.heads, a.r.n);
+  const dim3 grid((unsigned)((long)a.tiles * a.c.heads * a.r.n));
   const size_t lds = a.c.kind == CACHE_Q4 ? kTile * (a.c.dh / 8) * 4 : kTile * (a.c.dh / 2 + 1) * 4;
   if (a.c.kind == CACHE_Q4) hipLaunchKernelGGL(cache_write_kernel<CACHE_Q4>, grid, dim3(256), lds, s, a);
   else if (a.c.kind == CACHE_F16) hipLaunchKernelGGL(cache_write_kernel<CACHE_F16>, grid, dim3(256), lds, s, a);
@@ -634,7 +636,7 @@ hipError_t launch_cache_write(const CacheWriteArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 hipError_t launch_cache_read(const CacheReadArgs &a, hipStream_t s) {
-  const dim3 grid((a.max_keys + kTile - 1) / kTile, a.c.heads, a.r.n);
+  const dim3 grid((unsigned)((long)a.tiles * a.c.heads * a.r.n));
   const size_t lds = (a.c.kind == CACHE_Q4 ? 16 : 64) * a.c.dh;
   if (a.c.kind == CACHE_Q4) hipLaunchKernelGGL(cache_read_kernel<CACHE_Q4>, grid, dim3(256), lds, s, a);
   else if (a.c.kind == CACHE_F16) hipLaunchKernelGGL(cache_read_kernel<CACHE_F16>, grid, dim3(256), lds, s, a);
@@ -687,7 +689,7 @@ int check_config(const nt_cache_config *c) {
   if (c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128 && c->page_tokens != 256)
     return fail(NT_ESHAPE, "page_tokens %d not in {32,64,128,256}", c->page_tokens);
   if (c->n_pages < 1 || c->n_pages > 1 << 24) return fail(NT_ESHAPE, "n_pages must be in [1,2^24]");
-  if (c->max_seqs < 1 || c->max_seqs > 65535) return fail(NT_ESHAPE, "max_seqs must be in [1,65535]");
+  if (c->max_seqs < 1 || c->max_seqs > 1 << 20) return fail(NT_ESHAPE, "max_seqs must be in [1,2^20]");
   if (c->max_len < 1 || c->max_len > 1 << 24) return fail(NT_ESHAPE, "max_len must be in [1,2^24]");
   if ((double)c->n_layers * c->n_pages * c->page_tokens * c->n_kv_heads * c->d_head > 1e14) return fail(NT_ESHAPE, "the pool is beyond any memory");
   return NT_OK;
@@ -738,11 +740,11 @@ int type_bytes(int32_t type) { return type == NT_F32 ? 4 : 2; }
 bool type_known(int32_t type) { return type >= NT_F32 && type <= NT_BF16; }
 bool aligned(const void *p, int64_t ld, int32_t type) { return ((uintptr_t)p & 15) == 0 && (ld * type_bytes(type) & 15) == 0; }
 
-int write_rows(nt_cache *c, int32_t layer, const nt::CacheRows &r, const void *k, const void *v, int64_t ld, int32_t type, hipStream_t s) {
-  nt::CacheWriteArgs w{c->v, r, layer, type, k, v, ld, aligned(k, ld, type) && aligned(v, ld, type)};
-  HIP_TRY(nt::launch_cache_write(w, s));
-  return NT_OK;
+// workgroups of a launch: one dimension, below 2^31
+int check_blocks(int64_t tiles, int64_t heads, int64_t n) {
+  return (double)tiles * heads * n < 2147483648.0 ? NT_OK : fail(NT_ESHAPE, "%lld sequences of %lld tiles are too much for one call", (long long)n, (long long)tiles);
 }
+int write_tiles(int32_t max_new) { return (max_new + nt::kTile - 2) / nt::kTile + 1; }
 
 int become(nt_cache *c, int32_t n, const int32_t *d_src, const int32_t *d_dst, int deep, void *hip_stream) {
   int rc = check_call(c, n);
@@ -812,8 +814,7 @@ void nt_cache_destroy(nt_cache *c) {
 int nt_cache_reserve(nt_cache *c, int32_t n, const int32_t *d_seq, const int32_t *d_first, void *hip_stream) {
   int rc = check_call(c, n);
   if (rc || n == 0) return rc;
-  hipLaunchKernelGGL(nt::cache_reserve_kernel, dim3(1), dim3(nt::kPlan), 0, as_stream(hip_stream), c->v, nt::CacheRows{n, 0, d_seq, d_first}, c->w);
-  HIP_TRY(hipGetLastError());
+  HIP_TRY(nt::cache_reserve(c, nt::CacheRows{n, 0, d_seq, d_first}, as_stream(hip_stream)));
   return NT_OK;
 }
 
@@ -826,7 +827,9 @@ int nt_cache_write(nt_cache *c, int32_t layer, int32_t n, const int32_t *d_seq, 
   if (n == 0 || max_new == 0) return NT_OK;
   if (!d_k || !d_v) return fail(NT_EINVAL, "null argument");
   if (ld < (int64_t)c->cfg.n_kv_heads * c->cfg.d_head) return fail(NT_EINVAL, "row stride %lld shorter than a row", (long long)ld);
-  return write_rows(c, layer, nt::CacheRows{n, max_new, d_seq, d_first}, d_k, d_v, ld, type, as_stream(hip_stream));
+  if ((rc = check_blocks(write_tiles(max_new), c->cfg.n_kv_heads, n))) return rc;
+  HIP_TRY(nt::cache_write(c, layer, nt::CacheRows{n, max_new, d_seq, d_first}, d_k, d_v, ld, type, as_stream(hip_stream)));
+  return NT_OK;
 }
 
 int nt_cache_attend(nt_cache *c, const nt_attend_args *a, void *hip_stream) {
@@ -845,10 +848,11 @@ int nt_cache_attend(nt_cache *c, const nt_attend_args *a, void *hip_stream) {
   if (a->ld_q < (int64_t)g.n_q_heads * g.d_head || a->ld_out < (int64_t)g.n_q_heads * g.d_head ||
       (a->k && a->ld_kv < (int64_t)g.n_kv_heads * g.d_head))
     return fail(NT_EINVAL, "a row stride is shorter than a row");
-  hipStream_t s = as_stream(hip_stream);
-  const nt::CacheRows r{a->n, a->max_new, a->d_seq, a->d_first};
-  if (a->k && (rc = write_rows(c, a->layer, r, a->k, a->v, a->ld_kv, a->type, s))) return rc;
-  return nt::cache_attend(c, *a, a->type, 0, s);
+  if ((rc = check_blocks(((int64_t)a->max_new * (g.n_q_heads / g.n_kv_heads) + 7) / 8, g.n_kv_heads, a->n)) ||
+      (rc = check_blocks(write_tiles(a->max_new), g.n_kv_heads, a->n)))
+    return rc;
+  HIP_TRY(nt::cache_attend(c, *a, a->type, 0, as_stream(hip_stream)));
+  return NT_OK;
 }
 
 int nt_cache_read(nt_cache *c, int32_t layer, int32_t n, const int32_t *d_seq, int32_t max_keys, void *d_k, void *d_v, int32_t type,
@@ -859,7 +863,9 @@ int nt_cache_read(nt_cache *c, int32_t layer, int32_t n, const int32_t *d_seq, i
   if (max_keys < 0 || max_keys > 1 << 24) return fail(NT_ERANGE, "max_keys %d outside [0, 2^24]", max_keys);
   if (n == 0 || max_keys == 0) return NT_OK;
   if (!d_k || !d_v) return fail(NT_EINVAL, "null argument");
-  nt::CacheReadArgs r{c->v, nt::CacheRows{n, 0, d_seq, nullptr}, layer, type, max_keys, d_k, d_v};
+  const int tiles = (max_keys + nt::kTile - 1) / nt::kTile;
+  if ((rc = check_blocks(tiles, c->cfg.n_kv_heads, n))) return rc;
+  nt::CacheReadArgs r{c->v, nt::CacheRows{n, 0, d_seq, nullptr}, layer, type, max_keys, tiles, d_k, d_v};
   HIP_TRY(nt::launch_cache_read(r, as_stream(hip_stream)));
   return NT_OK;
 }
@@ -876,7 +882,7 @@ int nt_cache_truncate(nt_cache *c, int32_t n, const int32_t *d_seq, const int32_
   if (rc || n == 0) return rc;
   hipStream_t s = as_stream(hip_stream);
   if (!d_len) {
-    hipLaunchKernelGGL(nt::cache_end_kernel, dim3(n), dim3(256), 0, s, c->v, d_seq);
+    HIP_TRY(nt::cache_end(c, n, d_seq, s));
     if (d_seq) hipLaunchKernelGGL(nt::cache_unmark_kernel, dim3((n + 255) / 256), dim3(256), 0, s, c->v, n, d_seq);
   } else {
     hipLaunchKernelGGL(nt::cache_truncate_plan_kernel, dim3(1), dim3(nt::kPlan), 0, s, c->v, n, d_seq, d_len, c->w);
@@ -928,21 +934,38 @@ int nt_cache_check(nt_cache *c, void *hip_stream) {
 
 }  // extern "C"
 
+// ---- launches, for the entry points and the decoder -----------------------------------------------------------------------
+
+hipError_t nt::cache_reserve(nt_cache *c, const CacheRows &r, hipStream_t s) {
+  hipLaunchKernelGGL(cache_reserve_kernel, dim3(1), dim3(kPlan), 0, s, c->v, r, c->w);
+  return hipGetLastError();
+}
+hipError_t nt::cache_end(nt_cache *c, int n, const int32_t *seq, hipStream_t s) {
+  hipLaunchKernelGGL(cache_end_kernel, dim3(n), dim3(256), 0, s, c->v, seq);
+  return hipGetLastError();
+}
+hipError_t nt::cache_write(nt_cache *c, int layer, const CacheRows &r, const void *k, const void *v, long ld, int type, hipStream_t s) {
+  return launch_cache_write(CacheWriteArgs{c->v, r, layer, type, write_tiles(r.max_new), k, v, ld, aligned(k, ld, type) && aligned(v, ld, type)}, s);
+}
 // Attention by the kernel that fits
-int nt::cache_attend(nt_cache *c, const nt_attend_args &a, int out_type, long lo_offset, hipStream_t s) {
+hipError_t nt::cache_attend(nt_cache *c, const nt_attend_args &a, int out_type, long lo_offset, hipStream_t s) {
   const nt_cache_config &g = c->cfg;
-  nt::CacheAttnArgs k{};
-  k.c = c->v; k.r = nt::CacheRows{a.n, a.max_new, a.d_seq, a.d_first};
+  CacheAttnArgs k{};
+  k.c = c->v; k.r = CacheRows{a.n, a.max_new, a.d_seq, a.d_first};
+  if (a.k) {
+    const hipError_t e = cache_write(c, a.layer, k.r, a.k, a.v, a.ld_kv, a.type, s);
+    if (e != hipSuccess) return e;
+  }
   k.layer = a.layer; k.type = a.type; k.out_type = out_type; k.q_heads = g.n_q_heads; k.group = g.n_q_heads / g.n_kv_heads;
   k.q = a.q; k.out = a.out; k.ld_q = a.ld_q; k.ld_out = a.ld_out; k.lo_offset = lo_offset;
   k.scale = a.scale; k.window = a.window; k.sinks = a.sinks; k.vec = aligned(a.q, a.ld_q, a.type);
   k.part = c->part; k.count = c->count;
-  const long row_tiles = ((long)a.max_new * k.group + 7) / 8, blocks = row_tiles * g.n_kv_heads * a.n;
+  k.row_tiles = (int)(((long)a.max_new * k.group + 7) / 8);
+  const long blocks = (long)k.row_tiles * g.n_kv_heads * a.n;
   long keys = a.max_keys > 0 ? std::min(a.max_keys, g.max_len) : g.max_len;
   if (a.window > 0) keys = std::min<long>(keys, (long)a.window + a.sinks + a.max_new + 2 * kTile);
   const long tiles = (keys + kTile - 1) / kTile;
   // as many workgroups as the chip holds at once, none with less than a tile for each of its waves
-  k.splits = (int)std::max<long>(1, std::min({nt::kSplitBlocks / blocks, (tiles + 3) / 4, (long)nt::kMaxSplits}));
-  HIP_TRY(nt::launch_cache_token(k, (int)row_tiles, s));
-  return NT_OK;
+  k.splits = (int)std::max<long>(1, std::min({kSplitBlocks / blocks, (tiles + 3) / 4, (long)kMaxSplits}));
+  return launch_cache_token(k, s);
 }

@@ -15,7 +15,7 @@ namespace {
 constexpr int kRows = 8, kWaves = 4;
 
 template <int KIND, int DH>
-__global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a, int row_tiles) {
+__global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
   typedef typename FragType<KIND>::type F;
   typedef typename FragType<KIND>::elem E;
   constexpr int NC = DH / 32, NV = DH / 16, CH = DH < 256 ? DH : 256, LD = CH + 4;
@@ -25,13 +25,14 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a, int r
   __shared__ int lds_last;
   const CacheView &c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g4 = lane >> 4;
-  const int split = blockIdx.x % a.splits, h = blockIdx.x / a.splits % c.heads, rt = blockIdx.x / a.splits / c.heads, i = blockIdx.y;
+  const int split = blockIdx.x % a.splits, group = blockIdx.x / a.splits, h = group % c.heads, rt = group / c.heads % a.row_tiles,
+            i = group / c.heads / a.row_tiles;
   const int s = a.r.seq ? a.r.seq[i] : i;
   const long row0 = a.r.first ? a.r.first[i] : i;
   const int m = a.r.first ? a.r.first[i + 1] - (int)row0 : 1;
   const bool known = s >= 0 && s < c.max_seqs;
   const int len = known ? c.len[s] : 0, G = a.group, R = min(m, a.r.max_new) * G;
-  if ((!known || m < 0 || m > a.r.max_new || m > len) && blockIdx.x == 0 && tid == 0) atomicOr(c.flags, 1);
+  if ((!known || m < 0 || m > a.r.max_new || m > len) && split == 0 && h == 0 && rt == 0 && tid == 0) atomicOr(c.flags, 1);
   if (rt * kRows >= R) return;
   // positions of the rows, and the tiles that hold a key which one of them sees: those of the sinks, then those of the window
   const int first = len - m, p_min = first + rt * kRows / G, p_max = first + min(rt * kRows + kRows - 1, R - 1) / G;
@@ -154,7 +155,6 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a, int r
   sum = wave_pair32(sum, sum, WaveAdd{});
   if (lane < 8) lds_m[wave][lane] = top, lds_l[wave][lane] = sum;
 
-  const int group = (i * row_tiles + rt) * c.heads + h;
   float *part = a.part + (long)group * a.splits * kRows * (DH + 2);
   auto store = [&](int r, int d, float x, float l) {
     const int rr = rt * kRows + r;
@@ -224,22 +224,22 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a, int r
 }
 
 template <int KIND>
-hipError_t launch(const CacheAttnArgs &a, int row_tiles, hipStream_t s) {
-  const dim3 grid((unsigned)(a.splits * a.c.heads * row_tiles), (unsigned)a.r.n), block(256);
+hipError_t launch(const CacheAttnArgs &a, hipStream_t s) {
+  const dim3 grid((unsigned)((long)a.splits * a.c.heads * a.row_tiles * a.r.n)), block(256);
   switch (a.c.dh) {
-    case 64: hipLaunchKernelGGL((cache_token_kernel<KIND, 64>), grid, block, 0, s, a, row_tiles); break;
-    case 128: hipLaunchKernelGGL((cache_token_kernel<KIND, 128>), grid, block, 0, s, a, row_tiles); break;
-    case 256: hipLaunchKernelGGL((cache_token_kernel<KIND, 256>), grid, block, 0, s, a, row_tiles); break;
-    default: hipLaunchKernelGGL((cache_token_kernel<KIND, 512>), grid, block, 0, s, a, row_tiles);
+    case 64: hipLaunchKernelGGL((cache_token_kernel<KIND, 64>), grid, block, 0, s, a); break;
+    case 128: hipLaunchKernelGGL((cache_token_kernel<KIND, 128>), grid, block, 0, s, a); break;
+    case 256: hipLaunchKernelGGL((cache_token_kernel<KIND, 256>), grid, block, 0, s, a); break;
+    default: hipLaunchKernelGGL((cache_token_kernel<KIND, 512>), grid, block, 0, s, a);
   }
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_cache_token(const CacheAttnArgs &a, int row_tiles, hipStream_t s) {
-  if (a.c.kind == CACHE_Q4) return launch<CACHE_Q4>(a, row_tiles, s);
-  return a.c.kind == CACHE_F16 ? launch<CACHE_F16>(a, row_tiles, s) : launch<CACHE_BF16>(a, row_tiles, s);
+hipError_t launch_cache_token(const CacheAttnArgs &a, hipStream_t s) {
+  if (a.c.kind == CACHE_Q4) return launch<CACHE_Q4>(a, s);
+  return a.c.kind == CACHE_F16 ? launch<CACHE_F16>(a, s) : launch<CACHE_BF16>(a, s);
 }
 
 }  // namespace nt

@@ -3,8 +3,12 @@
 #include <hip/hip_runtime.h>
 
 #include "../../include/nt.h"
+#include "nt_cache.h"
 
 namespace nt {
-// nt_cache_attend after its checks, with k and v written; out_type: IoType, lo_offset: of the tails with IO_PLANES
-int cache_attend(nt_cache *c, const nt_attend_args &a, int out_type, long lo_offset, hipStream_t s);
+// The calls after their checks.  cache_attend, out_type: IoType, lo_offset: of the tails with IO_PLANES
+hipError_t cache_reserve(nt_cache *c, const CacheRows &r, hipStream_t s);
+hipError_t cache_end(nt_cache *c, int n, const int32_t *seq, hipStream_t s);  // seq: distinct ids, or the caller clears the marks
+hipError_t cache_write(nt_cache *c, int layer, const CacheRows &r, const void *k, const void *v, long ld, int type, hipStream_t s);
+hipError_t cache_attend(nt_cache *c, const nt_attend_args &a, int out_type, long lo_offset, hipStream_t s);
 }  // namespace nt

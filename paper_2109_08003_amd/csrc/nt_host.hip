@@ -17,6 +17,7 @@
 #include <vector>
 
 #include "../../include/nt.h"
+#include "nt_cache_host.h"
 #include "nt_kernels.h"
 
 // Scratch of nt_q8_output_layer_static: activation codes, per-row constants and arg-max partial keys for at most
@@ -217,7 +218,7 @@ struct nt_model {
   LN enc_final, dec_final;
   // device arena (one allocation)
   char *d_arena = nullptr;
-  size_t arena_bytes = 0;
+  size_t arena_bytes = 0, page_bytes = 0;
   float *x = nullptr;          // [Mt,d]  encoder residual stream
   void *a_enc = nullptr;       // [Mt,d]  LayerNorm output          (fp32 if kEncF32 else fp16)
   void *qkv = nullptr;         // [Mt,3d]
@@ -229,6 +230,8 @@ struct nt_model {
   // Single-head decoders of width 256 / 512 without relative keys keep both caches as 16-bit integers with one fp32
   // scale per vector (nt_dec1.hip): half the bytes of the fp32 self cache, and far less rounding than fp16.
   bool kv_i16 = false;
+  nt_cache *pages = nullptr;  // the self cache where it is paged (nt_config::self_cache), and
+  int32_t paged_rows = 0;     // how many of its sequences the last decode used
   // which encoder projections multiply the tail plane of their activations as well (bit 0: LayerNorm -> Q|K|V,
   // bit 1: attention context -> output projection, bit 2: final LayerNorm -> cross K|V, bit 3: the FFN's first matrix;
   // with bit 0 clear, bits 4 / 5 / 6: the q / k / v columns of Q|K|V alone; bit 7: q and k stored as plain fp16)
@@ -298,9 +301,15 @@ bool ffn_inside_layer(const nt_model *m, const DecLayer &L) {
   return m->kv_i16 && dec_ffn(&m->c) == m->c.d_model && L.ffn.W1_p != nullptr && L.ffn.W2_p != nullptr;
 }
 
-int check_config(const nt_config *c) {
-  if (!c) return fail(NT_EINVAL, "config is null");
-  if (c->struct_size != sizeof(nt_config)) return fail(NT_EINVAL, "config.struct_size %u != %zu", c->struct_size, sizeof(nt_config));
+// Checks *in and copies it to *out: fields behind its struct_size are 0 there.
+int check_config(const nt_config *in, nt_config *out) {
+  if (!in) return fail(NT_EINVAL, "config is null");
+  if (in->struct_size != sizeof(nt_config) && in->struct_size != offsetof(nt_config, self_cache))
+    return fail(NT_EINVAL, "config.struct_size %u != %zu", in->struct_size, sizeof(nt_config));
+  *out = nt_config{};
+  memcpy(out, in, in->struct_size);
+  out->struct_size = sizeof(nt_config);
+  const nt_config *c = out;
   if (c->n_enc < 0 || c->n_dec < 1 || c->vocab < 1 || c->n_heads < 1) return fail(NT_ESHAPE, "layer/vocab/head counts out of range");
   if (c->d_model < 64 || c->d_model > 1024 || c->d_model % 64) return fail(NT_ESHAPE, "d_model must be a multiple of 64 in [64,1024]");
   if (c->d_model % c->n_heads) return fail(NT_ESHAPE, "d_model not divisible by n_heads");
@@ -318,6 +327,10 @@ int check_config(const nt_config *c) {
   if (c->ln_l1 != 0 && c->ln_l1 != 1) return fail(NT_EINVAL, "ln_l1 must be 0 or 1");
   if (c->q8_output != 0 && c->q8_output != 1) return fail(NT_EINVAL, "q8_output must be 0 or 1");
   if (c->q8_output && !nt::vocab_q8_supported(c->d_model)) return fail(NT_ESHAPE, "the 8-bit output layer needs d_model 256 or 512");
+  if (c->self_cache != 0 && (c->self_cache < NT_CACHE_F16 || c->self_cache > NT_CACHE_Q4)) return fail(NT_EINVAL, "unknown self_cache %d", c->self_cache);
+  if (c->self_window < 0 || c->self_sinks < 0) return fail(NT_EINVAL, "negative self_window or self_sinks");
+  if (c->self_cache == 0 && (c->self_window || c->self_sinks)) return fail(NT_EINVAL, "self_window and self_sinks need a paged self_cache");
+  if (c->self_cache != 0 && c->rpr_clip > 0) return fail(NT_ESHAPE, "a paged self_cache has no relative position keys");
   if (c->pipeline_lanes < 0 || c->pipeline_lanes > 8 ) return fail(NT_EINVAL, "pipeline_lanes must be in [0,8]");
   return NT_OK;
 }
@@ -412,7 +425,7 @@ int alloc_lane_state(nt_model *m, hipStream_t s) {
   }
   std::vector<size_t> o_cross(cfg->n_dec), o_self(cfg->n_dec), o_cross_sc(cfg->n_dec), o_self_sc(cfg->n_dec);
   for (int l = 0; l < cfg->n_dec; l++) o_cross[l] = cv.take((size_t)Mt * 2 * d * (m->kv_i16 ? 2 : kCrossElt));
-  for (int l = 0; l < cfg->n_dec; l++) o_self[l] = cv.take((size_t)m->self_positions * 2 * d * (m->kv_i16 ? 2 : 4));
+  for (int l = 0; l < cfg->n_dec; l++) o_self[l] = cv.take(cfg->self_cache ? 16 : (size_t)m->self_positions * 2 * d * (m->kv_i16 ? 2 : 4));
   for (int l = 0; l < cfg->n_dec; l++) o_cross_sc[l] = cv.take(m->kv_i16 ? (size_t)Mt * (cfg->n_dec == 1 ? 4 : 2) * 4 : 16);
   for (int l = 0; l < cfg->n_dec; l++) o_self_sc[l] = cv.take(m->kv_i16 ? (size_t)m->self_positions * 2 * 4 : 16);
   const size_t o_z = cv.take((size_t)Br * d * 4), o_a32 = cv.take((size_t)Br * d * 4), o_q32 = cv.take((size_t)Br * d * 4),
@@ -452,6 +465,17 @@ int alloc_lane_state(nt_model *m, hipStream_t s) {
   m->q8_codes = at<int8_t>(A, o_q8c); m->q8_scale = at<float>(A, o_q8s); m->q8_c = at<int32_t>(A, o_q8z);
   m->q8_sa = at<int32_t>(A, o_q8a);
   m->scout_codes = at<int8_t>(A, o_sco); m->scout_rc = at<float4>(A, o_scr); m->scout_scratch = A + o_scs;
+  if (cfg->self_cache) {  // pages for every batch that check_decode_args lets pass: rows * steps positions, and one page a row that is not full
+    nt_cache_config g{};
+    g.struct_size = sizeof g; g.kind = cfg->self_cache; g.n_layers = cfg->n_dec; g.n_q_heads = g.n_kv_heads = dec_heads(cfg);
+    g.d_head = d / g.n_q_heads; g.page_tokens = nt::kTile; g.max_len = cfg->max_len;
+    const int64_t pages = m->self_positions / nt::kTile + Br;
+    if (Br > 1 << 20 || pages > 1 << 24) return fail(NT_ESHAPE, "a paged self_cache holds at most 2^20 rows and 2^24 pages");
+    g.max_seqs = (int32_t)Br; g.n_pages = (int32_t)pages;
+    const int rc = nt_cache_create(&g, s, &m->pages);
+    if (rc) return rc;
+    m->page_bytes = (size_t)nt_cache_bytes(&g);
+  }
   HIP_TRY(hipMemsetAsync(m->d_arena, 0, m->arena_bytes, s));  // load time only: no kernel ever reads an undefined word
   for (auto &st : m->stage) {
     if (hipHostMalloc((void **)&st.h_src, (size_t)Mt * 4) != hipSuccess || hipHostMalloc((void **)&st.h_len, (size_t)Br * 4) != hipSuccess ||
@@ -477,8 +501,9 @@ extern "C" {
 const char *nt_last_error(void) { return g_err.c_str(); }
 
 int64_t nt_param_count(const nt_config *cfg) {
-  if (check_config(cfg) != NT_OK) return 0;
-  return param_count(cfg);
+  nt_config c;
+  if (check_config(cfg, &c) != NT_OK) return 0;
+  return param_count(&c);
 }
 
 int32_t nt_n_steps(int32_t len) { return (6 * len + 4) / 5 + 2; }
@@ -519,8 +544,8 @@ int nt_debug_set_cert_distrust(nt_model *m, int on) {
 
 int64_t nt_device_bytes(const nt_model *m) {
   if (!m) return 0;
-  int64_t n = (int64_t)(m->w_bytes + m->table_bytes + m->scout_bytes + m->arena_bytes);
-  for (const nt_model *ln : m->lanes) n += (int64_t)ln->arena_bytes;
+  int64_t n = (int64_t)(m->w_bytes + m->table_bytes + m->scout_bytes + m->arena_bytes + m->page_bytes);
+  for (const nt_model *ln : m->lanes) n += (int64_t)(ln->arena_bytes + ln->page_bytes);
   return n;
 }
 
@@ -542,6 +567,7 @@ void nt_free(nt_model *m) {
   if (m->d_table && m->owns_weights) (void)hipFree(m->d_table);
   if (m->Wscout && m->owns_weights) (void)hipFree(m->Wscout);
   if (m->d_arena) (void)hipFree(m->d_arena);
+  nt_cache_destroy(m->pages);
   for (auto &st : m->stage) {
     if (st.done) (void)hipEventDestroy(st.done);
     if (st.h_src) (void)hipHostFree(st.h_src);
@@ -608,11 +634,13 @@ int spread_lane_streams(nt_model *m) {
 
 }  // namespace
 
-int nt_load_weights(const nt_config *cfg, const void *h_blob_fp16, size_t blob_bytes, void *hip_stream,
+int nt_load_weights(const nt_config *config, const void *h_blob_fp16, size_t blob_bytes, void *hip_stream,
                     nt_model **out) try {
   if (!out) return fail(NT_EINVAL, "out is null");
   *out = nullptr;
-  int rc = check_config(cfg);
+  nt_config full;
+  const nt_config *const cfg = &full;
+  int rc = check_config(config, &full);
   if (rc) return rc;
   if (!h_blob_fp16) return fail(NT_EINVAL, "blob is null");
   const int64_t np = param_count(cfg);
@@ -631,7 +659,7 @@ int nt_load_weights(const nt_config *cfg, const void *h_blob_fp16, size_t blob_b
   m->c = *cfg;
   m->max_tokens = cfg->max_batch_tokens;
   m->max_rows = cfg->max_batch_rows > 0 ? std::min<int64_t>(cfg->max_batch_rows, m->max_tokens) : m->max_tokens;
-  m->kv_i16 = nt::attn_i16_supported(cfg->d_model, dec_heads(cfg), cfg->rpr_clip);
+  m->kv_i16 = cfg->self_cache == 0 && nt::attn_i16_supported(cfg->d_model, dec_heads(cfg), cfg->rpr_clip);
   m->enc_tails = (cfg->n_heads == 1 && cfg->d_ffn == 0) ? kEncTailsStudent : kEncTailsAll;
   hipStream_t s = as_stream(hip_stream);
 
@@ -657,7 +685,7 @@ int nt_load_weights(const nt_config *cfg, const void *h_blob_fp16, size_t blob_b
   // self-attention: Wq|Wk|Wv fused into one [3d][d] matrix; cross-attention: Wq and Wk|Wv; fold: what folded batches need besides
   const bool fold_dec = m->kv_i16 && cfg->n_dec == 1;
   // The first decoder layer's Q | K | V comes from a table (Dec1Table); what it is made of: matrix [d][parts d] and bias, in double
-  const bool tabled = m->kv_i16 || (!kCrossF32 && nt::dec1_heads_supported(d, dec_heads(cfg)));
+  const bool tabled = m->kv_i16 || (cfg->self_cache == 0 && !kCrossF32 && nt::dec1_heads_supported(d, dec_heads(cfg)));
   // Larger batches fold their caches, too (CrossFold), but not before the 8-bit output layer: that the integers then round other vectors
   // moves a state by 2e-5, one of its codes every few steps, and 0.9 % of the tokens of 25-token sentences (all near-ties; 0.05 % with
   // the fp16 output layer).  (That is the distance of the two forms; which of them is nearer to exact arithmetic has not been measured.)
@@ -1123,8 +1151,12 @@ int decode_step(nt_model *m, DecodeCursor &cu, hipStream_t s) {
     const bool fused = nt::dec_fused_supported(d) && (m->dec_table.rows != nullptr || m->dec[0].self.Wqkv_p != nullptr);
     const bool fused_start = fused && rows_now > 0;
     // decoder layers whose attention half is one launch (nt_dec1.hip): the integer caches, or eight heads of 64
-    const bool heads_layer = !m->kv_i16 && fused && !kCrossF32 && nt::dec1_heads_supported(d, H);
+    const bool heads_layer = !m->kv_i16 && !m->pages && fused && !kCrossF32 && nt::dec1_heads_supported(d, H);
     const bool layer1 = m->kv_i16 || heads_layer;
+    if (m->pages && t == 0) {  // the sequences of the last decode end
+      if (m->paged_rows > 0) HIP_TRY(nt::cache_end(m->pages, m->paged_rows, nullptr, s));
+      m->paged_rows = B;
+    }
     // the EOS mode keeps the rows still decoding as a dense prefix: origin maps a dense row to its batch row
     int32_t *origin = eos ? m->origin[t & 1] : nullptr;
     if (eos) {
@@ -1159,6 +1191,8 @@ int decode_step(nt_model *m, DecodeCursor &cu, hipStream_t s) {
     const int R = rows_now;
     const double Rd = (double)R;
     // source tokens attended by the active rows (exact when the host knows the lengths)
+    const nt::CacheRows page_rows{R, 1, origin, nullptr};
+    if (m->pages) HIP_TRY(nt::cache_reserve(m->pages, page_rows, s));
     const double cross_keys = (m->len_prefix.size() > (size_t)R) ? (double)m->len_prefix[(size_t)R] : Rd * S;
     // One decoder projection: C = [LayerNorm](A) * Wt^T with the given epilogue.  Small row counts
     // take the one-round-trip kernel with the LayerNorm fused into its prologue.
@@ -1223,7 +1257,7 @@ int decode_step(nt_model *m, DecodeCursor &cu, hipStream_t s) {
         e.bias = L.self.bqkv; e.scale = qscale; e.scale_cols = d; e.dst0 = m->q32; e.ld0 = d; e.n_split = d;
         e.dst1 = m->self_kv[l] + (long)t * 2 * d; e.ld1 = self_stride;
         // the EOS mode and the integer caches: the pair goes to kv_new and the attention kernel appends it to the cache
-        if (eos || layer1) { e.dst1 = m->kv_new; e.ld1 = 2 * d; }
+        if (eos || layer1 || m->pages) { e.dst1 = m->kv_new; e.ld1 = 2 * d; }
         // the first layer's projection starts the step: by table inside the layer's launch, or in one with the embedding
         const bool by_table = l == 0 && layer1;
         nt::StepBeginArgs start = sba;
@@ -1283,10 +1317,19 @@ int decode_step(nt_model *m, DecodeCursor &cu, hipStream_t s) {
           }
           continue;
         }
-        KT(K_ATTN_DEC_SELF, Rd * (t + 1) * 2 * dd * 4 + Rd * dd * 8, 4 * Rd * (t + 1) * dd,
-           nt::launch_attn_decode(m->q32, m->self_kv[l], true, self_stride, nullptr, t + 1, R, d, H, L.self.rk,
-                                  c.rpr_clip, t, m->ctx32, s, streams(d, d, L.self.Wo_p, false) ? lo_rows * d : 0, origin,
-                                  eos ? m->kv_new : nullptr));
+        const long ctx_lo = streams(d, d, L.self.Wo_p, false) ? lo_rows * d : 0;
+        if (m->pages) {
+          nt_attend_args pa{};
+          pa.layer = l; pa.n = R; pa.max_new = 1; pa.max_keys = t + 1; pa.type = NT_F32; pa.window = c.self_window; pa.sinks = c.self_sinks;
+          pa.scale = 1.f; pa.d_seq = origin; pa.q = m->q32; pa.ld_q = pa.ld_out = d; pa.out = m->ctx32;
+          pa.k = m->kv_new; pa.v = m->kv_new + d; pa.ld_kv = 2 * d;
+          KT(K_ATTN_DEC_SELF, Rd * (t + 1) * 2 * (c.self_cache == NT_CACHE_Q4 ? dd * 17 / 32 : dd * 2) + Rd * dd * 16, 4 * Rd * (t + 1) * dd,
+             nt::cache_attend(m->pages, pa, ctx_lo ? nt::IO_PLANES : nt::IO_F32, ctx_lo, s));
+        } else {
+          KT(K_ATTN_DEC_SELF, Rd * (t + 1) * 2 * dd * 4 + Rd * dd * 8, 4 * Rd * (t + 1) * dd,
+             nt::launch_attn_decode(m->q32, m->self_kv[l], true, self_stride, nullptr, t + 1, R, d, H, L.self.rk,
+                                    c.rpr_clip, t, m->ctx32, s, ctx_lo, origin, eos ? m->kv_new : nullptr));
+        }
         nt::GemmEpilogue o;
         o.bias = L.self.bo; o.resid = m->z; o.ldr = d; o.dst0 = m->z; o.ld0 = d; o.n_split = d;
         if (!fused && (rc = dec_gemm(K_GEMM_DEC_O, m->ctx32, d, L.self.Wo, L.self.Wo_p, d, nullptr, o))) return rc;

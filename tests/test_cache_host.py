@@ -29,7 +29,7 @@ def test_configurations(host):  # noqa: F811
     bad, good, null = host(CACHE + """
 bad = [(kw, create(**kw)[0], create(**kw)[1].value, int(L.nt_cache_bytes(C.byref(config(**kw))))) for kw in (
     dict(kind=0), dict(kind=4), dict(n_layers=0), dict(n_q_heads=3), dict(n_q_heads=1), dict(n_kv_heads=0), dict(d_head=96), dict(d_head=1024),
-    dict(page_tokens=16), dict(page_tokens=48), dict(page_tokens=512), dict(n_pages=0), dict(n_pages=1 << 25), dict(max_seqs=0), dict(max_seqs=65536),
+    dict(page_tokens=16), dict(page_tokens=48), dict(page_tokens=512), dict(n_pages=0), dict(n_pages=1 << 25), dict(max_seqs=0), dict(max_seqs=1 << 21),
     dict(max_len=0), dict(max_len=1 << 25), dict(n_pages=1 << 24, page_tokens=256, n_layers=1024, n_kv_heads=4))]
 good = [(k, d, p, create(kind=k, d_head=d, page_tokens=p)[0], int(L.nt_cache_bytes(C.byref(config(kind=k, d_head=d, page_tokens=p)))))
         for k in (1, 2, 3) for d in (64, 128, 256, 512) for p in (32, 64, 128, 256)]
@@ -102,3 +102,43 @@ print(json.dumps(out))
             assert 0 < blocks < 2 ** 31, (name, blocks)
         write = [b for name, b in launches if "cache_write" in name]
         assert write == [((new + 30) // 32 + 1) * 2 * n]
+
+
+def test_models_with_a_paged_self_cache(host):  # noqa: F811
+    """Refusals, the configuration without the three fields (an older caller), device memory, and which launches a step makes."""
+    codes, older, sizes, steps = host("""
+from paper_2109_08003_amd.binding import NtConfig, lib, make_config
+def rc(**kw):
+    c, h = make_config(config(**kw), 4096), C.c_void_p()
+    blob = np.zeros(int(lib().nt_param_count(C.byref(make_config(config(), 4096)))), dtype=np.float16)
+    return lib().nt_load_weights(C.byref(c), blob.ctypes.data, blob.nbytes, None, C.byref(h))
+codes = [rc(self_cache=4), rc(self_cache=-1), rc(self_window=5), rc(self_sinks=1), rc(self_cache="q4", self_window=-1), rc(self_cache="f16", self_sinks=-1)]
+try:
+    codes.append(load(config(self_cache="f16", rpr_clip=4)))
+except nt.NtError as e:
+    codes.append(e.code)
+except AssertionError:
+    codes.append("no blob")
+c, h = make_config(config(), 4096), C.c_void_p()
+c.struct_size = NtConfig.self_cache.offset
+c.self_cache = 77                        # behind the caller's struct
+blob = np.zeros(int(lib().nt_param_count(C.byref(c))), dtype=np.float16)
+older = [lib().nt_load_weights(C.byref(c), blob.ctypes.data, blob.nbytes, None, C.byref(h)), c.self_cache, blob.size == nt.param_count(config())]
+sizes = [load(config(self_cache=k, self_window=20), tokens=2048).device_bytes() for k in ("f16", "bf16", "q4")]
+model = load(config(self_cache="q4", self_window=9, self_sinks=2, n_dec=2))
+encode(model, 3, 10)
+out = np.zeros((3, 5), dtype=np.int32)
+steps = []
+for _ in range(2):
+    stub.stub_clear()
+    nt.binding._check(lib().nt_decode_greedy(model._h, 3, 5, None, out.ctypes.data, None))
+    names = [n for n, b in launches()]
+    steps.append([sum(w in n for n in names) for w in ("cache_end", "cache_reserve", "cache_write", "cache_token", "dec1_kernel")])
+print(json.dumps((codes, older, sizes, steps)))
+""")
+    assert codes == [-1, -1, -1, -1, -1, -1, -2]
+    assert older == [0, 77, True]
+    positions = (6 * 2048 + 4) // 5 + 3 * 2048 + 8
+    pages = positions // 32 + 2048
+    assert sizes[0] == sizes[1] and sizes[0] - sizes[2] == pages * 32 * 2 * (512 * 2 - 512 // 2 - 512 // 32)
+    assert steps == [[0, 5, 10, 10, 0], [1, 5, 10, 10, 0]]
