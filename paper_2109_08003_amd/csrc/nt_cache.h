@@ -80,10 +80,9 @@ struct CacheAttnArgs {
   int32_t vec;     // query rows are 16-byte aligned
   int32_t row_tiles, splits;  // tiles of 8 query rows of a sequence, workgroups that share their keys
   float *part;     // [workgroup][8 queries][dh + 2]
-  int32_t *count;  // [workgroup / splits], zero between calls
 };
 constexpr int kSplitBlocks = 1024;  // workgroups among which split keys are spread, at most
-constexpr int kMaxSplits = 64;      // of one row: the last workgroup reads what the others left
+constexpr int kMaxSplits = 64;      // of one row: a workgroup of the join reads them all
 // Queries in tiles of 8 (rows: token, then head of the group), each split over the keys.  Any number of rows.
 hipError_t launch_cache_token(const CacheAttnArgs &a, hipStream_t s);
 

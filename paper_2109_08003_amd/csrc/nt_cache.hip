@@ -464,13 +464,12 @@ __global__ __launch_bounds__(kPlan) void cache_lengths_kernel(CacheView c, int32
   }
 }
 
-__global__ __launch_bounds__(256) void cache_clear_kernel(CacheView c, int32_t *count, int n_count) {
+__global__ __launch_bounds__(256) void cache_clear_kernel(CacheView c) {
   const long i = (long)blockIdx.x * 256 + threadIdx.x, words = (c.n_pages + 31) / 32;
   if (i < c.max_seqs) c.len[i] = c.base[i] = 0, c.slot[i] = -1, c.mark[i] = INT_MAX;
   if (i < c.n_pages) c.ref[i] = 0;
   if (i < words) c.used[i] = i * 32 + 32 <= c.n_pages ? 0 : ~((1u << (c.n_pages & 31)) - 1);  // bits behind the last page: never free
   if (i < 2) c.flags[i] = 0;
-  if (i < n_count) count[i] = 0;
 }
 
 // ---- values in and out ------------------------------------------------------------------------------------------------
@@ -655,7 +654,6 @@ struct nt_cache {
   int device = -1;
   char *mem = nullptr;
   float *part = nullptr;
-  int32_t *count = nullptr;
   int32_t *h_flags = nullptr;  // pinned
 };
 
@@ -719,7 +717,6 @@ size_t lay_out(nt_cache *c, char *base) {
   c->w.off = ints(g.max_seqs); c->w.list = ints(g.n_pages); c->w.from = ints(g.n_pages); c->w.to = ints(g.n_pages);
   c->w.info = ints(2); c->w.row_len = ints(g.max_seqs); c->w.row = ints((size_t)g.max_seqs * v.width);
   c->part = (float *)take((size_t)nt::kSplitBlocks * 8 * (g.d_head + 2) * 4);
-  c->count = ints(nt::kSplitBlocks);
   return off;
 }
 
@@ -789,8 +786,8 @@ int nt_cache_create(const nt_cache_config *cfg, void *hip_stream, nt_cache **out
       return fail(NT_ENOMEM, "pinned allocation failed");
     }
     lay_out(c, c->mem);
-    const int most = std::max(std::max(cfg->n_pages, cfg->max_seqs), nt::kSplitBlocks);
-    hipLaunchKernelGGL(nt::cache_clear_kernel, dim3((most + 255) / 256), dim3(256), 0, as_stream(hip_stream), c->v, c->count, nt::kSplitBlocks);
+    const int most = std::max(cfg->n_pages, cfg->max_seqs);
+    hipLaunchKernelGGL(nt::cache_clear_kernel, dim3((most + 255) / 256), dim3(256), 0, as_stream(hip_stream), c->v);
     HIP_TRY(hipGetLastError());
     HIP_TRY(hipStreamSynchronize(as_stream(hip_stream)));
     return NT_OK;
@@ -959,7 +956,7 @@ hipError_t nt::cache_attend(nt_cache *c, const nt_attend_args &a, int out_type, 
   k.layer = a.layer; k.type = a.type; k.out_type = out_type; k.q_heads = g.n_q_heads; k.group = g.n_q_heads / g.n_kv_heads;
   k.q = a.q; k.out = a.out; k.ld_q = a.ld_q; k.ld_out = a.ld_out; k.lo_offset = lo_offset;
   k.scale = a.scale; k.window = a.window; k.sinks = a.sinks; k.vec = aligned(a.q, a.ld_q, a.type);
-  k.part = c->part; k.count = c->count;
+  k.part = c->part;
   k.row_tiles = (int)(((long)a.max_new * k.group + 7) / 8);
   const long blocks = (long)k.row_tiles * g.n_kv_heads * a.n;
   long keys = a.max_keys > 0 ? std::min(a.max_keys, g.max_len) : g.max_len;
