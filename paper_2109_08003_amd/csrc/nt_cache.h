@@ -77,7 +77,7 @@ struct CacheAttnArgs {
   long ld_q, ld_out, lo_offset;
   float scale;
   int32_t window, sinks;
-  int32_t vec;     // query rows are 16-byte aligned
+  int32_t vec, vec_out;  // query rows, output rows are 16-byte aligned
   int32_t row_tiles, splits;  // tiles of 8 query rows of a sequence, workgroups that share their keys
   float *part;     // [workgroup][8 queries][dh + 2]
 };
@@ -85,6 +85,8 @@ constexpr int kSplitBlocks = 1024;  // workgroups among which split keys are spr
 constexpr int kMaxSplits = 64;      // of one row: a workgroup of the join reads them all
 // Queries in tiles of 8 (rows: token, then head of the group), each split over the keys.  Any number of rows.
 hipError_t launch_cache_token(const CacheAttnArgs &a, hipStream_t s);
+// Tiles of 128 to 256 query rows, unsplit; row_tiles, splits and part are not used.
+hipError_t launch_cache_prompt(const CacheAttnArgs &a, hipStream_t s);
 
 #ifdef __HIPCC__
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));

@@ -1,0 +1,392 @@
+// Attention of many rows over a paged cache: prompts.
+//
+// A workgroup has a tile of query rows of one key/value head (rows: token, then head of the group) and walks the keys that they
+// see, a stage of tiles at a time: all its waves take part in bringing the next stage to the LDS (16-bit tiles as they are, by loads
+// that go there directly; 4-bit ones rounded back to fp16 once for all waves) while each computes on the present one for its own
+// NQ x 16 rows, with the running maximum and sum of the softmax in registers.  As in the kernel for few rows, scores are S^T = K Q^T
+// and weights enter O^T = V^T P^T from the registers they are made in.
+#include "nt_cache_frag.h"
+
+namespace nt {
+namespace {
+
+typedef __attribute__((address_space(3))) char lds_char;
+
+// Rows of a wave in tiles of 16, waves, tiles of keys in a stage.  Accumulators, queries, scores and weights of a wave are
+// NQ (DH / 4 + DH / 8 + 12) registers, 256 for two waves per SIMD; a fragment read from the LDS serves NQ products of 16 clocks,
+// and four SIMDs can read one in 32.
+template <int DH> struct PromptShape { static constexpr int NQ = 1, NW = 8, ST = 1; };
+template <> struct PromptShape<64> { static constexpr int NQ = 4, NW = 4, ST = 2; };
+template <> struct PromptShape<128> { static constexpr int NQ = 3, NW = 4, ST = 2; };
+template <> struct PromptShape<256> { static constexpr int NQ = 2, NW = 4, ST = 1; };
+
+// 0xFFFF in the halves of w that are infinities or NaN: their exponent is all ones, and one more carries into the sign
+template <typename E>
+__device__ __forceinline__ uint32_t no_numbers(uint32_t w) {
+  constexpr uint32_t one = __is_same(E, _Float16) ? 0x04000400u : 0x00800080u;
+  const uint32_t b = ((w & 0x7FFF7FFFu) + one) & 0x80008000u;
+  return (b << 1) - (b >> 15);
+}
+
+constexpr float kSlack = 8.f;  // log2 by which a weight may exceed 1 before sums and accumulators are rescaled
+
+template <int KIND, int DH>
+__global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_kernel(CacheAttnArgs a, int spread) {
+  typedef typename FragType<KIND>::type F;
+  typedef typename FragType<KIND>::elem E;
+  constexpr int NQ = PromptShape<DH>::NQ, NW = PromptShape<DH>::NW, ST = PromptShape<DH>::ST;
+  constexpr int NC = DH / 32, NV = DH / 16, TB = 128 * DH, ROWS = NW * NQ * 16;
+  extern __shared__ __align__(1024) char lds[];  // [2][ST][TB]
+  const CacheView &c = a.c;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g4 = lane >> 4, G = a.group;
+  // row tiles of a head's sequence follow one another on one of the eight dies, whose cache they share; long ones first
+  const int b = blockIdx.x, j = spread ? b / 8 : b;
+  const int unit = spread ? j / a.row_tiles * 8 + b % 8 : j / a.row_tiles, rt = a.row_tiles - 1 - j % a.row_tiles;
+  const int h = unit % c.heads, i = unit / c.heads;
+  if (i >= a.r.n) return;
+  const int s = a.r.seq ? a.r.seq[i] : i;
+  const long row0 = a.r.first ? a.r.first[i] : i;
+  const int m = a.r.first ? a.r.first[i + 1] - (int)row0 : 1;
+  const bool known = s >= 0 && s < c.max_seqs;
+  const int len = known ? c.len[s] : 0, R = min(m, a.r.max_new) * G;
+  if ((!known || m < 0 || m > a.r.max_new || m > len) && h == 0 && rt == 0 && tid == 0) atomicOr(c.flags, 1);
+  if (rt * ROWS >= R) return;
+  // as Share in the kernel for few rows
+  const int first = len - m, p_min = first + rt * ROWS / G, p_max = first + min(rt * ROWS + ROWS - 1, R - 1) / G;
+  const int low = a.window > 0 ? max(p_min - a.window + 1, 0) : 0;
+  const int sink_tiles = (min(a.sinks, low) + kTile - 1) / kTile, window_tile = max(low / kTile, sink_tiles);
+  const int tiles = p_max < 0 ? 0 : sink_tiles + max(p_max / kTile + 1 - window_tile, 0), stages = (tiles + ST - 1) / ST;
+  auto tile_of = [&](int t) { return t < sink_tiles ? t : window_tile + t - sink_tiles; };
+
+  // queries: rounded to the cache's type in the LDS, in the order in which the waves read them back.  A power of two brings the
+  // largest of each to 1 .. 2: no overflow in fp16.
+  __shared__ float lds_scale[ROWS];
+#pragma unroll 1
+  for (int x = tid; x < ROWS * DH / 8; x += NW * 64) {
+    const int r = x / (DH / 8), d = x % (DH / 8) * 8, row = rt * ROWS + r, tok = row / G;
+    float v[8] = {}, big = 0.f;
+    if (row < R) io_load8(a.q, a.type, (row0 + tok) * a.ld_q + (long)(h * G + row % G) * DH + d, a.vec, v);
+#pragma unroll
+    for (int k = 0; k < 8; k++) big = fmaxf(big, fabsf(v[k]));
+#pragma unroll
+    for (int k = 1; k < DH / 8; k *= 2) big = fmaxf(big, __shfl_xor(big, k, 64));
+    const int ex = big > 0.f && big < __builtin_inff() ? min(max(ilogbf(big), -100), 126) : 0;
+    if (d == 0) lds_scale[r] = ldexpf(fabsf(a.scale) * 1.44269504088896f, ex);
+    const float down = ldexpf(a.scale < 0.f ? -1.f : 1.f, -ex);
+    F f;
+#pragma unroll
+    for (int k = 0; k < 8; k++) f[k] = (E)(v[k] * down);
+    ((F *)lds)[(r / 16 * NC + d / 32) * 64 + d / 8 % 4 * 16 + r % 16] = f;
+  }
+  __syncthreads();
+  const int wave_row = rt * ROWS + wave * NQ * 16;
+  F q[NQ][NC];
+  float to_log2[NQ];
+  int pos[NQ];
+#pragma unroll
+  for (int k = 0; k < NQ; k++) {
+    const int row = wave_row + k * 16 + col;
+    pos[k] = row < R ? first + row / G : -1;
+    to_log2[k] = lds_scale[row - rt * ROWS];
+#pragma unroll
+    for (int e = 0; e < NC; e++) q[k][e] = ((const F *)lds)[((wave * NQ + k) * NC + e) * 64 + lane];
+  }
+  __syncthreads();
+  // positions of the wave's rows
+  const int w_min = wave_row < R ? first + wave_row / G : 0, w_max = wave_row < R ? first + min(wave_row + NQ * 16 - 1, R - 1) / G : -1;
+  const int w_low = a.window > 0 ? max(w_min - a.window + 1, 0) : 0;
+
+  const int sub_bits = c.page_shift - 5;
+  const int32_t *table = c.table + (long)s * c.width;
+  const char *layer = c.pool + a.layer * c.layer_bytes;
+  constexpr int kBytes = KIND == CACHE_Q4 ? 34 * DH : TB;
+  auto page_of = [&](int t) { return t < tiles ? table[tile_of(t) >> sub_bits] : -1; };
+  auto address = [&](int t, int page) {
+    return layer + page * c.page_bytes + (long)((h << sub_bits) + (tile_of(t) & ((1 << sub_bits) - 1))) * kBytes;
+  };
+
+  // pieces of a 4-bit tile that a wave brings: 16 bytes a lane, four fragments
+  constexpr int PIECES = DH / 32, MINE = KIND == CACHE_Q4 ? (ST * PIECES + NW - 1) / NW : 1;
+  uint4 code[MINE];
+  uint32_t sc[MINE][4];
+  auto fetch = [&](int stage, const int (&page)[ST], int buf) {
+#pragma unroll
+    for (int x = 0; x < ST; x++) {
+      if (page[x] < 0) continue;
+      const char *at = address(stage * ST + x, page[x]);
+      if constexpr (KIND != CACHE_Q4) {
+        for (int k = wave; k < TB / 1024; k += NW)
+          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(at + k * 1024 + lane * 16),
+                                           (__attribute__((address_space(3))) void *)(lds + (buf * ST + x) * TB + k * 1024), 16, 0, 0);
+      }
+    }
+    if constexpr (KIND == CACHE_Q4) {
+#pragma unroll
+      for (int y = 0; y < MINE; y++) {
+        const int piece = wave + y * NW, x = piece / PIECES, p = piece % PIECES;
+        int pg = -1;
+#pragma unroll
+        for (int z = 0; z < ST; z++)
+          if (x == z) pg = page[z];
+        if (pg < 0) continue;
+        const char *at = address(stage * ST + x, pg);
+        code[y] = *(const uint4 *)(at + p * 1024 + lane * 16);
+        if (p < PIECES / 2) {  // keys: words 4 p .. 4 p + 3
+          const int tok = 8 * (col >> 2) + (col & 3);
+          const char *scales = at + 32 * DH;
+          if constexpr (NC == 2) {
+            sc[y][0] = *(const unsigned short *)(scales + tok * NC);
+            sc[y][1] = *(const unsigned short *)(scales + (tok + 4) * NC);
+          } else {
+            const int t = 4 * p / NC;
+            sc[y][0] = *(const uint32_t *)(scales + (tok + 4 * t) * NC + 4 * p % NC);
+          }
+        } else {
+          const char *scales = at + 33 * DH + (p - PIECES / 2) * 2 * kTile + g4 * 8;
+          const uint2 u = *(const uint2 *)scales, v = *(const uint2 *)(scales + kTile);
+          sc[y][0] = u.x, sc[y][1] = u.y, sc[y][2] = v.x, sc[y][3] = v.y;
+        }
+      }
+    }
+  };
+  auto place = [&](uint32_t there, int buf) {  // 4 bits: what fetch left in registers
+    if constexpr (KIND == CACHE_Q4) {
+#pragma unroll
+      for (int y = 0; y < MINE; y++) {
+        const int piece = wave + y * NW, x = piece / PIECES, p = piece % PIECES;
+        if (!(there >> x & 1)) continue;
+        char *to = lds + (buf * ST + x) * TB + p * 4096 + lane * 16;
+#pragma unroll
+        for (int w = 0; w < 4; w++) {
+          f16x2 v[4];
+          q4_unpack(((const uint32_t *)&code[y])[w], v);
+          if (p < PIECES / 2) {
+            const uint32_t by = (NC == 2 ? sc[y][w / 2] >> (8 * (w % 2)) : sc[y][0] >> (8 * w)) & 0xFF;
+            const f16x2 f = __builtin_bit_cast(f16x2, by << 8 | by << 24);
+#pragma unroll
+            for (int d = 0; d < 4; d++) v[d] *= f;
+          } else {
+#pragma unroll
+            for (int d = 0; d < 4; d++) v[d] *= q4_scale_pair(sc[y][w / 2 * 2 + d / 2], d % 2);
+          }
+          *(f16x8 *)(to + w * 1024) = q4_join(v);
+        }
+      }
+    }
+  };
+
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  f32x4 o[NQ][NV];
+  float top[NQ], sum[NQ];
+#pragma unroll
+  for (int k = 0; k < NQ; k++) {
+    top[k] = -__builtin_inff();
+    sum[k] = 0.f;
+#pragma unroll
+    for (int n = 0; n < NV; n++) o[k][n] = zero;
+  }
+
+  int next[ST];
+  uint32_t present = 0, present_next = 0;  // bit x: tile x of the stage has a page
+  auto look_up = [&](int stage) {
+#pragma unroll
+    for (int x = 0; x < ST; x++) next[x] = page_of(stage * ST + x);
+  };
+  auto mask_of = [&]() {
+    uint32_t b = 0;
+#pragma unroll
+    for (int x = 0; x < ST; x++) b |= (next[x] >= 0 ? 1u : 0u) << x;
+    return b;
+  };
+  look_up(0);
+  present = mask_of();
+  fetch(0, next, 0);
+  place(present, 0);
+  look_up(1);
+  bool strange = false;  // values that are no numbers were left out of a tile that not all rows see
+  __syncthreads();
+  for (int stage = 0; stage < stages; stage++) {
+    const int buf = stage & 1;
+    present_next = mask_of();
+    fetch(stage + 1, next, buf ^ 1);
+    look_up(stage + 2);
+#pragma unroll 1
+    for (int x = 0; x < ST; x++) {
+      const int j0 = tile_of(stage * ST + x) * kTile;
+      // nothing for this wave
+      if (!(present >> x & 1) || j0 > w_max || (j0 + kTile <= w_low && j0 >= a.sinks)) continue;
+      const bool all_seen = j0 + kTile - 1 <= w_min && (a.window == 0 || j0 >= w_max - a.window + 1 || j0 + kTile <= a.sinks);
+      const F *keys = (const F *)(lds + (buf * ST + x) * TB) + lane, *values = keys + 4 * DH;
+      f32x4 y[NQ][2];
+#pragma unroll
+      for (int k = 0; k < NQ; k++) y[k][0] = y[k][1] = zero;
+#pragma unroll
+      for (int t = 0; t < 2; t++)
+#pragma unroll
+        for (int e = 0; e < NC; e++) {
+          const F kf = keys[(t * NC + e) * 64];
+#pragma unroll
+          for (int k = 0; k < NQ; k++) y[k][t] = mma(kf, q[k][e], y[k][t]);
+        }
+      if (!all_seen) {
+#pragma unroll
+        for (int k = 0; k < NQ; k++) {
+          const int from = a.window > 0 ? pos[k] - a.window + 1 : 0;
+#pragma unroll
+          for (int d = 0; d < 8; d++) {
+            const int key = j0 + g4 * 8 + d;
+            y[k][d / 4][d % 4] = (key > pos[k]) | ((key < from) & (key >= a.sinks)) ? -__builtin_inff() : y[k][d / 4][d % 4];
+          }
+        }
+      }
+      F p[NQ];
+#pragma unroll
+      for (int k = 0; k < NQ; k++) {
+        float mx = y[k][0][0];
+#pragma unroll
+        for (int d = 1; d < 8; d++) mx = fmaxf(mx, y[k][d / 4][d % 4]);
+        mx = wave_pair16(mx, mx, WaveMax{});
+        mx = wave_pair32(mx, mx, WaveMax{}) * to_log2[k];
+        if (__any(mx > top[k] + kSlack)) {  // the rows that need it: a row does not depend on its neighbours
+          const float up = mx > top[k] + kSlack ? mx : top[k], shrink = __builtin_amdgcn_exp2f(top[k] - (up == -__builtin_inff() ? 0.f : up));
+          top[k] = up;
+          sum[k] *= shrink;
+#pragma unroll
+          for (int n = 0; n < NV; n++) o[k][n] *= shrink;
+        }
+        const float from = top[k] == -__builtin_inff() ? 0.f : top[k];
+        float add = 0.f;
+#pragma unroll
+        for (int d = 0; d < 8; d++) {
+          const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(y[k][d / 4][d % 4], to_log2[k], -from));
+          add += z;
+          p[k][d] = (E)z;
+        }
+        sum[k] += add;
+      }
+      if (all_seen) {
+#pragma unroll
+        for (int n = 0; n < NV; n++) {
+          const F vf = values[n * 64];
+#pragma unroll
+          for (int k = 0; k < NQ; k++) o[k][n] = mma(vf, p[k], o[k][n]);
+        }
+      } else {
+        uint32_t keep[4];  // keys that some row of the wave sees
+#pragma unroll
+        for (int d = 0; d < 4; d++) {
+          const int key = j0 + g4 * 8 + 2 * d;
+          keep[d] = ((key <= w_max) & ((key >= w_low) | (key < a.sinks)) ? 0xFFFFu : 0) |
+                    ((key + 1 <= w_max) & ((key + 1 >= w_low) | (key + 1 < a.sinks)) ? 0xFFFF0000u : 0);
+        }
+#pragma unroll
+        for (int n = 0; n < NV; n++) {
+          uint4 raw = __builtin_bit_cast(uint4, values[n * 64]);
+          raw.x &= keep[0], raw.y &= keep[1], raw.z &= keep[2], raw.w &= keep[3];
+          const uint32_t bad = no_numbers<E>(raw.x) | no_numbers<E>(raw.y) | no_numbers<E>(raw.z) | no_numbers<E>(raw.w);
+          if (__any(bad != 0)) {
+            strange = true;
+            raw.x &= ~no_numbers<E>(raw.x), raw.y &= ~no_numbers<E>(raw.y), raw.z &= ~no_numbers<E>(raw.z), raw.w &= ~no_numbers<E>(raw.w);
+          }
+          const F vf = __builtin_bit_cast(F, raw);
+#pragma unroll
+          for (int k = 0; k < NQ; k++) o[k][n] = mma(vf, p[k], o[k][n]);
+        }
+      }
+    }
+    place(present_next, buf ^ 1);
+    present = present_next;
+    __syncthreads();
+  }
+#pragma unroll
+  for (int k = 0; k < NQ; k++) {
+    const int row = wave_row + k * 16 + col;
+    float l = wave_pair16(sum[k], sum[k], WaveAdd{});
+    l = wave_pair32(l, l, WaveAdd{});
+    if (row >= R) continue;
+    const long at = (row0 + row / G) * a.ld_out + (long)(h * G + row % G) * DH + g4 * 4;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    auto rows = [&](auto *out) {
+      typedef std::remove_pointer_t<decltype(out)> T;
+      typedef T T4 __attribute__((ext_vector_type(4)));
+      if (a.vec_out) {
+#pragma unroll
+        for (int n = 0; n < NV; n++) {
+          T4 v;
+#pragma unroll
+          for (int d = 0; d < 4; d++) v[d] = (T)(l == 0.f ? 0.f : o[k][n][d] * inv);
+          *(T4 *)(out + at + n * 16) = v;
+        }
+      } else {
+#pragma unroll
+        for (int n = 0; n < NV; n++)
+#pragma unroll
+          for (int d = 0; d < 4; d++) out[at + n * 16 + d] = (T)(l == 0.f ? 0.f : o[k][n][d] * inv);
+      }
+    };
+    if (a.out_type == IO_F32) rows((float *)a.out);
+    else if (a.out_type == IO_F16) rows((_Float16 *)a.out);
+    else rows((__bf16 *)a.out);
+  }
+  if (!strange) return;
+  // Infinities and NaN among the values of tiles that not all rows of the wave see: they reach the rows that see them.  A lane
+  // corrects what it has stored.
+  for (int t = 0; t < tiles; t++) {
+    const int pg = page_of(t), j0 = tile_of(t) * kTile;
+    const bool all_seen = j0 + kTile - 1 <= w_min && (a.window == 0 || j0 >= w_max - a.window + 1 || j0 + kTile <= a.sinks);
+    if (pg < 0 || all_seen || j0 > w_max || (j0 + kTile <= w_low && j0 >= a.sinks)) continue;
+    const char *at = address(t, pg);
+    for (int key = 0; key < kTile; key++)
+      for (int x = 0; x < DH / 4; x++) {
+        const int dim = x / 4 * 16 + g4 * 4 + x % 4;
+        float v;
+        if constexpr (KIND == CACHE_Q4) {
+          v = q4_scale(((const unsigned char *)at)[33 * DH + dim / 32 * kTile + key]);
+          if (v == v) continue;
+        } else {
+          v = (float)((const E *)(at + 64 * DH))[value_elem(key, dim)];
+          if (v - v == 0.f) continue;
+        }
+        for (int k = 0; k < NQ; k++) {
+          const int row = wave_row + k * 16 + col, p = row < R ? first + row / G : -1;
+          if (j0 + key > p || (a.window > 0 && j0 + key < p - a.window + 1 && j0 + key >= a.sinks)) continue;
+          const long o = (row0 + row / G) * a.ld_out + (long)(h * G + row % G) * DH + dim;
+          io_store(a.out, a.out_type, o, 0, io_load(a.out, a.out_type, o) + v);
+        }
+      }
+  }
+}
+
+template <int KIND, int DH>
+hipError_t launch(CacheAttnArgs a, hipStream_t s) {
+  typedef PromptShape<DH> P;
+  constexpr int kLds = 2 * P::ST * 128 * DH, kRows = P::NW * P::NQ * 16;
+  static const hipError_t limit = hipFuncSetAttribute((const void *)cache_prompt_kernel<KIND, DH>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+  if (limit != hipSuccess) return limit;
+  a.row_tiles = (int)(((long)a.r.max_new * a.group + kRows - 1) / kRows);
+  const long units = (long)a.r.n * a.c.heads;
+  // spread over the dies by unit where that leaves none idle
+  const int spread = units % 8 == 0 || units >= 64;
+  const long blocks = (spread ? (units + 7) / 8 * 8 : units) * a.row_tiles;
+  hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH>), dim3((unsigned)blocks), dim3(P::NW * 64), kLds, s, a, spread);
+  return hipGetLastError();
+}
+
+template <int KIND>
+hipError_t launch_width(const CacheAttnArgs &a, hipStream_t s) {
+  switch (a.c.dh) {
+    case 64: return launch<KIND, 64>(a, s);
+    case 128: return launch<KIND, 128>(a, s);
+    case 256: return launch<KIND, 256>(a, s);
+    default: return launch<KIND, 512>(a, s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_cache_prompt(const CacheAttnArgs &a, hipStream_t s) {
+  if (a.c.kind == CACHE_Q4) return launch_width<CACHE_Q4>(a, s);
+  return a.c.kind == CACHE_F16 ? launch_width<CACHE_F16>(a, s) : launch_width<CACHE_BF16>(a, s);
+}
+
+}  // namespace nt
