@@ -5,6 +5,8 @@
 // that go there directly; 4-bit ones rounded back to fp16 once for all waves) while each computes on the present one for its own
 // NQ x 16 rows, with the running maximum and sum of the softmax in registers.  As in the kernel for few rows, scores are S^T = K Q^T
 // and weights enter O^T = V^T P^T from the registers they are made in.
+#include <climits>
+
 #include "nt_cache_frag.h"
 
 namespace nt {
@@ -16,8 +18,8 @@ typedef __attribute__((address_space(3))) char lds_char;
 // NQ (DH / 4 + DH / 8 + 12) registers, 256 for two waves per SIMD; a fragment read from the LDS serves NQ products of 16 clocks,
 // and four SIMDs can read one in 32.
 template <int DH> struct PromptShape { static constexpr int NQ = 1, NW = 8, ST = 1; };
-template <> struct PromptShape<64> { static constexpr int NQ = 4, NW = 4, ST = 2; };
-template <> struct PromptShape<128> { static constexpr int NQ = 3, NW = 4, ST = 2; };
+template <> struct PromptShape<64> { static constexpr int NQ = 2, NW = 4, ST = 1; };
+template <> struct PromptShape<128> { static constexpr int NQ = 3, NW = 4, ST = 1; };
 template <> struct PromptShape<256> { static constexpr int NQ = 2, NW = 4, ST = 1; };
 
 // 0xFFFF in the halves of w that are infinities or NaN: their exponent is all ones, and one more carries into the sign
@@ -28,7 +30,8 @@ __device__ __forceinline__ uint32_t no_numbers(uint32_t w) {
   return (b << 1) - (b >> 15);
 }
 
-constexpr float kSlack = 8.f;  // log2 by which a weight may exceed 1 before sums and accumulators are rescaled
+constexpr float kSlack = 8.f;     // log2 by which a weight may exceed 1 before sums and accumulators are rescaled
+constexpr float kLowest = -1e38f;  // maximum of no score; less than any that is a number
 
 template <int KIND, int DH>
 __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_kernel(CacheAttnArgs a, int spread) {
@@ -36,7 +39,7 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
   typedef typename FragType<KIND>::elem E;
   constexpr int NQ = PromptShape<DH>::NQ, NW = PromptShape<DH>::NW, ST = PromptShape<DH>::ST;
   constexpr int NC = DH / 32, NV = DH / 16, TB = 128 * DH, ROWS = NW * NQ * 16;
-  extern __shared__ __align__(1024) char lds[];  // [2][ST][TB]
+  extern __shared__ __align__(1024) char lds[];  // [2][ST][TB], before that the queries
   const CacheView &c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g4 = lane >> 4, G = a.group;
   // row tiles of a head's sequence follow one another on one of the eight dies, whose cache they share; long ones first
@@ -61,6 +64,8 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
   // queries: rounded to the cache's type in the LDS, in the order in which the waves read them back.  A power of two brings the
   // largest of each to 1 .. 2: no overflow in fp16.
   __shared__ float lds_scale[ROWS];
+  __shared__ int lds_strange;  // values that are no numbers were left out
+  if (tid == 0) lds_strange = 0;
 #pragma unroll 1
   for (int x = tid; x < ROWS * DH / 8; x += NW * 64) {
     const int r = x / (DH / 8), d = x % (DH / 8) * 8, row = rt * ROWS + r, tok = row / G;
@@ -180,7 +185,7 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
   float top[NQ], sum[NQ];
 #pragma unroll
   for (int k = 0; k < NQ; k++) {
-    top[k] = -__builtin_inff();
+    top[k] = kLowest;
     sum[k] = 0.f;
 #pragma unroll
     for (int n = 0; n < NV; n++) o[k][n] = zero;
@@ -203,13 +208,39 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
   fetch(0, next, 0);
   place(present, 0);
   look_up(1);
-  bool strange = false;  // values that are no numbers were left out of a tile that not all rows see
+  // whether all rows of the workgroup see all keys of a tile
+  auto seen_by_all = [&](int j0) { return j0 + kTile - 1 <= p_min && (a.window == 0 || j0 >= p_max - a.window + 1 || j0 + kTile <= a.sinks); };
+  // Where they do not, the values of keys that none sees, and those that are no numbers, become zero in the LDS before the product.
+  auto clean = [&](int j0, char *tile) {
+    for (int k = tid; k < NV * 64; k += NW * 64) {
+      uint4 *at = (uint4 *)(tile + 64 * DH) + k, v = *at;
+      uint32_t *w = (uint32_t *)&v, bad = 0;
+#pragma unroll
+      for (int d = 0; d < 4; d++) {
+        const int key = j0 + (k & 63) / 16 * 8 + 2 * d;
+        w[d] &= ((key <= p_max) & ((key >= low) | (key < a.sinks)) ? 0xFFFFu : 0) |
+                ((key + 1 <= p_max) & ((key + 1 >= low) | (key + 1 < a.sinks)) ? 0xFFFF0000u : 0);
+        bad |= no_numbers<E>(w[d]);
+        w[d] &= ~no_numbers<E>(w[d]);
+      }
+      if (bad) lds_strange = 1;
+      *at = v;
+    }
+  };
   __syncthreads();
   for (int stage = 0; stage < stages; stage++) {
     const int buf = stage & 1;
     present_next = mask_of();
     fetch(stage + 1, next, buf ^ 1);
     look_up(stage + 2);
+    bool cleaned = false;
+    for (int x = 0; x < ST; x++) {
+      const int j0 = tile_of(stage * ST + x) * kTile;
+      if (!(present >> x & 1) || stage * ST + x >= tiles || seen_by_all(j0)) continue;
+      clean(j0, lds + (buf * ST + x) * TB);
+      cleaned = true;
+    }
+    if (cleaned) __syncthreads();
 #pragma unroll 1
     for (int x = 0; x < ST; x++) {
       const int j0 = tile_of(stage * ST + x) * kTile;
@@ -242,56 +273,43 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
       F p[NQ];
 #pragma unroll
       for (int k = 0; k < NQ; k++) {
-        float mx = y[k][0][0];
+        float z[8];
+        auto weigh = [&]() {
+          int big = INT_MIN;
 #pragma unroll
-        for (int d = 1; d < 8; d++) mx = fmaxf(mx, y[k][d / 4][d % 4]);
-        mx = wave_pair16(mx, mx, WaveMax{});
-        mx = wave_pair32(mx, mx, WaveMax{}) * to_log2[k];
-        if (__any(mx > top[k] + kSlack)) {  // the rows that need it: a row does not depend on its neighbours
-          const float up = mx > top[k] + kSlack ? mx : top[k], shrink = __builtin_amdgcn_exp2f(top[k] - (up == -__builtin_inff() ? 0.f : up));
+          for (int d = 0; d < 8; d++) {
+            z[d] = __builtin_fmaf(y[k][d / 4][d % 4], to_log2[k], -top[k]);
+            big = max(big, __float_as_int(z[d]));  // of positive numbers the largest
+          }
+          return big;
+        };
+        if (__any(weigh() > __float_as_int(kSlack))) {  // some row: those that need it change their maximum, no other row depends on them
+          float mx = y[k][0][0];
+#pragma unroll
+          for (int d = 1; d < 8; d++) mx = fmaxf(mx, y[k][d / 4][d % 4]);
+          mx = wave_pair16(mx, mx, WaveMax{});
+          mx = wave_pair32(mx, mx, WaveMax{}) * to_log2[k];
+          const float up = mx - top[k] > kSlack ? mx : top[k], shrink = __builtin_amdgcn_exp2f(top[k] - up);
           top[k] = up;
           sum[k] *= shrink;
 #pragma unroll
           for (int n = 0; n < NV; n++) o[k][n] *= shrink;
+          weigh();
         }
-        const float from = top[k] == -__builtin_inff() ? 0.f : top[k];
         float add = 0.f;
 #pragma unroll
         for (int d = 0; d < 8; d++) {
-          const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(y[k][d / 4][d % 4], to_log2[k], -from));
-          add += z;
-          p[k][d] = (E)z;
+          const float x = __builtin_amdgcn_exp2f(z[d]);
+          add += x;
+          p[k][d] = (E)x;
         }
         sum[k] += add;
       }
-      if (all_seen) {
 #pragma unroll
-        for (int n = 0; n < NV; n++) {
-          const F vf = values[n * 64];
+      for (int n = 0; n < NV; n++) {
+        const F vf = values[n * 64];
 #pragma unroll
-          for (int k = 0; k < NQ; k++) o[k][n] = mma(vf, p[k], o[k][n]);
-        }
-      } else {
-        uint32_t keep[4];  // keys that some row of the wave sees
-#pragma unroll
-        for (int d = 0; d < 4; d++) {
-          const int key = j0 + g4 * 8 + 2 * d;
-          keep[d] = ((key <= w_max) & ((key >= w_low) | (key < a.sinks)) ? 0xFFFFu : 0) |
-                    ((key + 1 <= w_max) & ((key + 1 >= w_low) | (key + 1 < a.sinks)) ? 0xFFFF0000u : 0);
-        }
-#pragma unroll
-        for (int n = 0; n < NV; n++) {
-          uint4 raw = __builtin_bit_cast(uint4, values[n * 64]);
-          raw.x &= keep[0], raw.y &= keep[1], raw.z &= keep[2], raw.w &= keep[3];
-          const uint32_t bad = no_numbers<E>(raw.x) | no_numbers<E>(raw.y) | no_numbers<E>(raw.z) | no_numbers<E>(raw.w);
-          if (__any(bad != 0)) {
-            strange = true;
-            raw.x &= ~no_numbers<E>(raw.x), raw.y &= ~no_numbers<E>(raw.y), raw.z &= ~no_numbers<E>(raw.z), raw.w &= ~no_numbers<E>(raw.w);
-          }
-          const F vf = __builtin_bit_cast(F, raw);
-#pragma unroll
-          for (int k = 0; k < NQ; k++) o[k][n] = mma(vf, p[k], o[k][n]);
-        }
+        for (int k = 0; k < NQ; k++) o[k][n] = mma(vf, p[k], o[k][n]);
       }
     }
     place(present_next, buf ^ 1);
@@ -328,13 +346,11 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
     else if (a.out_type == IO_F16) rows((_Float16 *)a.out);
     else rows((__bf16 *)a.out);
   }
-  if (!strange) return;
-  // Infinities and NaN among the values of tiles that not all rows of the wave see: they reach the rows that see them.  A lane
-  // corrects what it has stored.
+  if (!lds_strange) return;
+  // The infinities and NaN that were left out reach the rows that see them: a lane corrects what it has stored.
   for (int t = 0; t < tiles; t++) {
     const int pg = page_of(t), j0 = tile_of(t) * kTile;
-    const bool all_seen = j0 + kTile - 1 <= w_min && (a.window == 0 || j0 >= w_max - a.window + 1 || j0 + kTile <= a.sinks);
-    if (pg < 0 || all_seen || j0 > w_max || (j0 + kTile <= w_low && j0 >= a.sinks)) continue;
+    if (pg < 0 || seen_by_all(j0)) continue;
     const char *at = address(t, pg);
     for (int key = 0; key < kTile; key++)
       for (int x = 0; x < DH / 4; x++) {
@@ -360,7 +376,8 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
 template <int KIND, int DH>
 hipError_t launch(CacheAttnArgs a, hipStream_t s) {
   typedef PromptShape<DH> P;
-  constexpr int kLds = 2 * P::ST * 128 * DH, kRows = P::NW * P::NQ * 16;
+  constexpr int kRows = P::NW * P::NQ * 16, kStages = 2 * P::ST * 128 * DH, kQueries = kRows * DH * 2;
+  constexpr int kLds = kStages > kQueries ? kStages : kQueries;  // first the queries, then the stages
   static const hipError_t limit = hipFuncSetAttribute((const void *)cache_prompt_kernel<KIND, DH>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
   if (limit != hipSuccess) return limit;
   a.row_tiles = (int)(((long)a.r.max_new * a.group + kRows - 1) / kRows);
