@@ -78,14 +78,15 @@ struct CacheAttnArgs {
   float scale;
   int32_t window, sinks;
   int32_t vec, vec_out;  // query rows, output rows are 16-byte aligned
-  int32_t row_tiles, splits;  // tiles of 8 query rows of a sequence, workgroups that share their keys
-  float *part;     // [workgroup][8 queries][dh + 2]
+  float *part;           // kSplitBlocks x 8 x (dh + 2)
+  // set by the launchers: tiles of query rows of a sequence, workgroups that share their keys
+  int32_t row_tiles, splits;
 };
 constexpr int kSplitBlocks = 1024;  // workgroups among which split keys are spread, at most
 constexpr int kMaxSplits = 64;      // of one row: a workgroup of the join reads them all
-// Queries in tiles of 8 (rows: token, then head of the group), each split over the keys.  Any number of rows.
-hipError_t launch_cache_token(const CacheAttnArgs &a, hipStream_t s);
-// Tiles of 128 to 256 query rows, unsplit; row_tiles, splits and part are not used.
+// Queries in tiles of 8 (rows: token, then head of the group), each split over the keys, of which a row sees about `tiles` tiles.
+hipError_t launch_cache_token(CacheAttnArgs a, long tiles, hipStream_t s);
+// Tiles of 128 to 256 query rows, unsplit.
 hipError_t launch_cache_prompt(const CacheAttnArgs &a, hipStream_t s);
 
 #ifdef __HIPCC__

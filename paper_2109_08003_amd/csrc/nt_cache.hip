@@ -957,13 +957,8 @@ hipError_t nt::cache_attend(nt_cache *c, const nt_attend_args &a, int out_type, 
   k.q = a.q; k.out = a.out; k.ld_q = a.ld_q; k.ld_out = a.ld_out; k.lo_offset = lo_offset;
   k.scale = a.scale; k.window = a.window; k.sinks = a.sinks; k.vec = aligned(a.q, a.ld_q, a.type); k.vec_out = aligned(a.out, a.ld_out, a.type);
   k.part = c->part;
-  k.row_tiles = (int)(((long)a.max_new * k.group + 7) / 8);
-  const long blocks = (long)k.row_tiles * g.n_kv_heads * a.n;
+  if ((long)a.max_new * k.group > 64) return launch_cache_prompt(k, s);
   long keys = a.max_keys > 0 ? std::min(a.max_keys, g.max_len) : g.max_len;
   if (a.window > 0) keys = std::min<long>(keys, (long)a.window + a.sinks + a.max_new + 2 * kTile);
-  const long tiles = (keys + kTile - 1) / kTile;
-  // as many workgroups as the chip holds at once, none with less than a tile for each of its waves
-  if ((long)a.max_new * k.group > 64) return launch_cache_prompt(k, s);
-  k.splits = (int)std::max<long>(1, std::min({kSplitBlocks / blocks, (tiles + 3) / 4, (long)kMaxSplits}));
-  return launch_cache_token(k, s);
+  return launch_cache_token(k, (keys + kTile - 1) / kTile, s);
 }

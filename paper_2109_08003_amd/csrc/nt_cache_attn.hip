@@ -6,12 +6,17 @@
 // instruction are eight queries twice: the head of the query (and of the weights) in the cache's type, and the tail against it, so that both
 // products have twice the bits at no cost: reading the keys and values is what such a call is bound by.
 // The waves meet in the LDS; where several workgroups share the keys of a row, a second launch joins what they left in memory.
+#include <algorithm>
+
 #include "nt_cache_frag.h"
 
 namespace nt {
 namespace {
 
 constexpr int kRows = 8, kWaves = 4;
+// Waves that share a tile, 128 dims each, and so tiles in work at a time: beyond 128 dims the accumulators, keys and values of a
+// wave would leave one wave to a SIMD.  Their parts of the scores are added through the LDS.
+constexpr int parts_of(int dh) { return dh > 128 ? dh / 128 : 1; }
 
 // What a workgroup has to do: the rows of sequence i in row tile rt, the tiles of keys that one of them sees (those of the sinks, then
 // those of the window), and how they are shared out.
@@ -21,7 +26,7 @@ struct Share {
   int first, p_min, p_max, low;            // positions: of the first new token, of the rows; first key of the earliest window
   int sink_tiles, window_tile, tiles, per, shares;
   bool known;
-  __device__ __forceinline__ Share(const CacheAttnArgs &a, int i, int rt) {
+  __device__ __forceinline__ Share(const CacheAttnArgs &a, int i, int rt, int at_once) {
     s = a.r.seq ? a.r.seq[i] : i;
     row0 = a.r.first ? a.r.first[i] : i;
     m = a.r.first ? a.r.first[i + 1] - (int)row0 : 1;
@@ -35,7 +40,7 @@ struct Share {
     sink_tiles = (min(a.sinks, low) + kTile - 1) / kTile;
     window_tile = max(low / kTile, sink_tiles);
     tiles = p_max < 0 ? 0 : sink_tiles + max(p_max / kTile + 1 - window_tile, 0);
-    per = max((tiles + a.splits - 1) / a.splits, kWaves);
+    per = max((tiles + a.splits - 1) / a.splits, at_once);
     shares = max((tiles + per - 1) / per, 1);
   }
 };
@@ -46,77 +51,106 @@ __device__ __forceinline__ void store_row(const CacheAttnArgs &a, const Share &w
     io_store(a.out, a.out_type, (w.row0 + row / a.group) * a.ld_out + (long)(h * a.group + row % a.group) * dh + d, a.lo_offset, l == 0.f ? 0.f : x / l);
 }
 
-template <int KIND, int DH>
+// ONE: every sequence has one new token, so the rows of a workgroup see the same keys
+template <int KIND, int DH, bool ONE>
 __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
   typedef typename FragType<KIND>::type F;
   typedef typename FragType<KIND>::elem E;
-  constexpr int NC = DH / 32, NV = DH / 16, CH = DH < 256 ? DH : 256, LD = CH + 4;
-  __shared__ float lds_o[kWaves][kRows][LD];
-  __shared__ float lds_m[kWaves][kRows], lds_l[kWaves][kRows];
+  constexpr int PARTS = parts_of(DH), GROUPS = kWaves / PARTS, DW = DH / PARTS, NC = DW / 32, NV = DW / 16;
+  __shared__ float lds_o[GROUPS][kRows][DH + 4];
+  __shared__ float lds_m[GROUPS][kRows], lds_l[GROUPS][kRows], lds_scale[kRows];
+  __shared__ f32x4 lds_s[PARTS > 1 ? 2 : 1][PARTS > 1 ? kWaves : 1][2][PARTS > 1 ? 64 : 1];
+  char *lds_q = (char *)lds_o;  // before the loop
+  static_assert(sizeof(lds_o) >= DH * 32, "");
   const CacheView &c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g4 = lane >> 4;
+  const int part = wave % PARTS, mine = wave / PARTS;  // of a tile's dims, of the tiles in work
   const int split = blockIdx.x % a.splits, group = blockIdx.x / a.splits, h = group % c.heads, rt = group / c.heads % a.row_tiles,
             i = group / c.heads / a.row_tiles;
-  const Share w(a, i, rt);
+  const Share w(a, i, rt, GROUPS);
   const int G = a.group;
   if ((!w.known || w.m < 0 || w.m > a.r.max_new || w.m > w.len) && split == 0 && h == 0 && rt == 0 && tid == 0) atomicOr(c.flags, 1);
   if (rt * kRows >= w.R || split >= w.shares) return;
   const int t1 = min((split + 1) * w.per, w.tiles);
 
-  // this lane's query: head g of the group in columns g and g + 8
-  const int row = rt * kRows + (col & 7), tok = row / G;
-  const bool real = row < w.R;
-  const int pos = real ? w.first + tok : -1, low_own = a.window > 0 ? pos - a.window + 1 : 0;
-  F q[NC];
-  float to_log2;
-  {
-    float x[NC][8], top = 0.f;
+  // the queries: heads of the group in columns 0 .. 7, their tails in 8 .. 15.  A power of two brings the largest of each to
+  // 1 .. 2: no overflow in fp16, and tails with all their bits.
+  for (int x = tid; x < kRows * DH / 8; x += 256) {
+    const int r = x / (DH / 8), d = x % (DH / 8) * 8, row = rt * kRows + r;
+    float v[8] = {}, big = 0.f;
+    if (row < w.R) io_load8(a.q, a.type, (w.row0 + row / G) * a.ld_q + (long)(h * G + row % G) * DH + d, a.vec, v);
 #pragma unroll
-    for (int k = 0; k < NC; k++) {
-      if (real) io_load8(a.q, a.type, (w.row0 + tok) * a.ld_q + (long)(h * G + row % G) * DH + k * 32 + g4 * 8, a.vec, x[k]);
+    for (int k = 0; k < 8; k++) big = fmaxf(big, fabsf(v[k]));
 #pragma unroll
-      for (int j = 0; j < 8; j++) {
-        if (!real) x[k][j] = 0.f;
-        top = fmaxf(top, fabsf(x[k][j]));
-      }
-    }
-    top = wave_pair16(top, top, WaveMax{});
-    top = wave_pair32(top, top, WaveMax{});
-    // a power of two brings the largest of the query to 1 .. 2: no overflow in fp16, and a tail with all its bits
-    const int e = top > 0.f && top < __builtin_inff() ? min(max(ilogbf(top), -100), 126) : 0;
-    to_log2 = ldexpf(a.scale * 1.44269504088896f, e);
+    for (int k = 1; k < DH / 8; k *= 2) big = fmaxf(big, __shfl_xor(big, k, 64));
+    const int e = big > 0.f && big < __builtin_inff() ? min(max(ilogbf(big), -100), 126) : 0;
+    if (d == 0) lds_scale[r] = ldexpf(a.scale * 1.44269504088896f, e);
     const float down = ldexpf(1.f, -e);
+    F head, tail;
 #pragma unroll
-    for (int k = 0; k < NC; k++)
-#pragma unroll
-      for (int j = 0; j < 8; j++) {
-        const float y = as_f32(x[k][j] * down);
-        const E head = (E)y;
-        q[k][j] = col < 8 ? head : (E)(y - (float)head);
-      }
+    for (int k = 0; k < 8; k++) {
+      const float y = as_f32(v[k] * down);
+      head[k] = (E)y;
+      tail[k] = (E)(y - (float)head[k]);
+    }
+    F *to = (F *)lds_q + d / 32 * 64 + d / 8 % 4 * 16 + r;
+    to[0] = head;
+    to[8] = tail;
   }
+  const int row = rt * kRows + (col & 7);
+  const int pos = row < w.R ? w.first + row / G : -1, low_own = a.window > 0 ? pos - a.window + 1 : 0;
+  // the wave's first tile is on its way before the queries are there
+  const int sub_bits = c.page_shift - 5;
+  const int32_t *table = c.table + (long)w.s * c.width;
+  auto tile_of = [&](int t) { return t < w.sink_tiles ? t : w.window_tile + t - w.sink_tiles; };
+  auto page_of = [&](int t) { return t < t1 ? table[tile_of(t) >> sub_bits] : -1; };
+  auto address = [&](int t, int page) {  // of a page that is not there: the first one's tile, which is then not looked at
+    return c.pool + cache_tile_offset(c, a.layer, max(page, 0), h, tile_of(t) & ((1 << sub_bits) - 1), cache_tile_bytes(KIND, DH));
+  };
+  KeyTile<KIND, DH, DW> kt;
+  ValueTile<KIND, DH, DW> vt;
+  int t = split * w.per + mine;
+  int page = page_of(t), page_next = page_of(t + GROUPS);
+  if (t < t1) {
+    const char *at = address(t, page);
+    kt.load(at, lane, part);
+    vt.load(at, lane, part);
+  }
+  __syncthreads();
+  F q[NC];
+#pragma unroll
+  for (int k = 0; k < NC; k++) q[k] = ((const F *)lds_q)[(part * NC + k) * 64 + lane];
+  const float to_log2 = lds_scale[col & 7];
 
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   f32x4 o[NV];
 #pragma unroll
   for (int n = 0; n < NV; n++) o[n] = zero;
   float top = -__builtin_inff(), sum = 0.f;
-  const int sub_bits = c.page_shift - 5;
-  const int32_t *table = c.table + (long)w.s * c.width;
-  for (int t = split * w.per + wave; t < t1; t += kWaves) {
-    const int tile = t < w.sink_tiles ? t : w.window_tile + t - w.sink_tiles;
-    const int page = table[tile >> sub_bits];
-    if (page < 0) continue;
-    const char *at = c.pool + cache_tile_offset(c, a.layer, page, h, tile & ((1 << sub_bits) - 1), cache_tile_bytes(KIND, DH));
-    KeyTile<KIND, DH> kt;
-    ValueTile<KIND, DH> vt;
-    kt.load(at, lane);
-    vt.load(at, lane);
+  int turn = 0;
+  for (; PARTS > 1 ? t - mine < t1 : t < t1; t += GROUPS) {  // waves that meet make the same number of turns
+    const int j0 = tile_of(t) * kTile;
     f32x4 sc[2] = {zero, zero};
 #pragma unroll
     for (int k = 0; k < NC; k++) {
       sc[0] = mma(kt.frag(0, k), q[k], sc[0]);
       sc[1] = mma(kt.frag(1, k), q[k], sc[1]);
+    }
+    // the next tile's keys take the place of these, its values that of these after the second product
+    const char *next = address(min(t + GROUPS, t1 - 1), page_next);
+    if (t + GROUPS < t1) kt.load(next, lane, part);
+    const int page_after = page_of(t + 2 * GROUPS);
+    if constexpr (PARTS > 1) {
+      lds_s[turn][wave][0][lane] = sc[0];
+      lds_s[turn][wave][1][lane] = sc[1];
+      __syncthreads();
+      sc[0] = sc[1] = zero;
+#pragma unroll
+      for (int k = 0; k < PARTS; k++) {
+        sc[0] += lds_s[turn][mine * PARTS + k][0][lane];
+        sc[1] += lds_s[turn][mine * PARTS + k][1][lane];
+      }
+      turn ^= 1;
     }
     float y[8];
 #pragma unroll
@@ -124,8 +158,8 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
       const float x = sc[j / 4][j % 4];
       y[j] = (x + __uint_as_float(wave_dpp<0x128>(__float_as_uint(x)))) * to_log2;  // head and tail: columns 8 apart
     }
-    const int j0 = tile * kTile;
-    const bool all_seen = j0 + kTile - 1 <= w.p_min && (a.window == 0 || j0 >= w.p_max - a.window + 1 || j0 + kTile <= a.sinks);
+    const bool all_seen =
+        page >= 0 && j0 + kTile - 1 <= w.p_min && (a.window == 0 || j0 >= w.p_max - a.window + 1 || j0 + kTile <= a.sinks);
     uint32_t seen = 0xFF;
     if (!all_seen) {
       uint32_t someone = 0;
@@ -133,9 +167,11 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; j++) {
         const int key = j0 + g4 * 8 + j;
-        if (key <= pos && (key >= low_own || key < a.sinks)) seen |= 1u << j;
-        else y[j] = -__builtin_inff();
-        if (key <= w.p_max && (key >= w.low || key < a.sinks)) someone |= 1u << j;
+        const bool own = (page >= 0) & (key <= pos) & ((key >= low_own) | (key < a.sinks));
+        const bool any = (page >= 0) & (key <= w.p_max) & ((key >= w.low) | (key < a.sinks));
+        seen |= (own ? 1u : 0u) << j;
+        someone |= (any ? 1u : 0u) << j;
+        y[j] = own ? y[j] : -__builtin_inff();
       }
       vt.clear(someone);
     }
@@ -144,9 +180,9 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
     for (int j = 1; j < 8; j++) tile_top = fmaxf(tile_top, y[j]);
     tile_top = wave_pair16(tile_top, tile_top, WaveMax{});
     tile_top = wave_pair32(tile_top, tile_top, WaveMax{});
-    const float next = fmaxf(top, tile_top), from = next == -__builtin_inff() ? 0.f : next;
+    const float up = fmaxf(top, tile_top), from = up == -__builtin_inff() ? 0.f : up;
     const float shrink = __builtin_amdgcn_exp2f(top - from);
-    top = next;
+    top = up;
     sum *= shrink;
     F p;
 #pragma unroll
@@ -159,54 +195,54 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
 #pragma unroll
     for (int n = 0; n < NV; n++) o[n] *= shrink;
     bool bad = false;
-    if (!all_seen && w.p_min < w.p_max) {  // rows of different tokens: some see keys that others do not
+    if (!ONE && !all_seen && w.p_min < w.p_max) {  // rows of different tokens: some see keys that others do not
 #pragma unroll
       for (int n = 0; n < NV; n++) bad |= any_no_number(vt.frag(n));
     }
-    if (__any(bad)) {
+    if (!ONE && __any(bad)) {
 #pragma unroll
       for (int n = 0; n < NV; n++) o[n] = mma_seen(vt.frag(n), p, seen, o[n]);
     } else {
 #pragma unroll
       for (int n = 0; n < NV; n++) o[n] = mma(vt.frag(n), p, o[n]);
     }
+    if (t + GROUPS < t1) vt.load(next, lane, part);
+    page = page_next;
+    page_next = page_after;
   }
   sum = wave_pair16(sum, sum, WaveAdd{});
   sum = wave_pair32(sum, sum, WaveAdd{});
-  if (lane < 8) lds_m[wave][lane] = top, lds_l[wave][lane] = sum;
 
-  float *part = a.part + ((long)group * a.splits + split) * kRows * (DH + 2);
+  const long at = (long)group * a.splits + split;  // [workgroup][row][dim], then [workgroup][row] {maximum, sum}
+  __syncthreads();                                 // the last use of the LDS
+  if (lane < 8 && part == 0) lds_m[mine][lane] = top, lds_l[mine][lane] = sum;
 #pragma unroll
-  for (int d0 = 0; d0 < DH; d0 += CH) {
-    __syncthreads();
+  for (int n = 0; n < NV; n++) {
+    f32x4 x = o[n];
 #pragma unroll
-    for (int n = 0; n < CH / 16; n++) {
-      f32x4 x = o[d0 / 16 + n];
+    for (int k = 0; k < 4; k++) x[k] += __uint_as_float(wave_dpp<0x128>(__float_as_uint(x[k])));
+    if (col < 8) *(f32x4 *)&lds_o[mine][col][part * DW + n * 16 + g4 * 4] = x;
+  }
+  __syncthreads();
+  for (int x = tid; x < kRows * DH; x += 256) {
+    const int r = x / DH, d = x % DH;
+    if (rt * kRows + r >= w.R) break;
+    float mx = lds_m[0][r];
 #pragma unroll
-      for (int k = 0; k < 4; k++) x[k] += __uint_as_float(wave_dpp<0x128>(__float_as_uint(x[k])));
-      if (col < 8) *(f32x4 *)&lds_o[wave][col][n * 16 + g4 * 4] = x;
+    for (int k = 1; k < GROUPS; k++) mx = fmaxf(mx, lds_m[k][r]);
+    const float from = mx == -__builtin_inff() ? 0.f : mx;
+    float l = 0.f, y = 0.f;
+#pragma unroll
+    for (int k = 0; k < GROUPS; k++) {
+      const float f = __builtin_amdgcn_exp2f(lds_m[k][r] - from);
+      l += f * lds_l[k][r];
+      y += f * lds_o[k][r][d];
     }
-    __syncthreads();
-    for (int x = tid; x < kRows * CH; x += 256) {
-      const int r = x / CH, d = x % CH;
-      float mx = lds_m[0][r];
-#pragma unroll
-      for (int k = 1; k < kWaves; k++) mx = fmaxf(mx, lds_m[k][r]);
-      const float from = mx == -__builtin_inff() ? 0.f : mx;
-      float l = 0.f, y = 0.f;
-#pragma unroll
-      for (int k = 0; k < kWaves; k++) {
-        const float f = __builtin_amdgcn_exp2f(lds_m[k][r] - from);
-        l += f * lds_l[k][r];
-        y += f * lds_o[k][r][d];
-      }
-      if (w.shares == 1) {
-        store_row(a, w, h, rt * kRows + r, d0 + d, DH, y, l);
-      } else {
-        float *to = part + r * (DH + 2);
-        to[d0 + d] = y;
-        if (d0 + d == 0) to[DH] = mx, to[DH + 1] = l;
-      }
+    if (w.shares == 1) {
+      store_row(a, w, h, rt * kRows + r, d, DH, y, l);
+    } else {
+      a.part[(at * kRows + r) * DH + d] = y;
+      if (d == 0) ((float2 *)(a.part + (long)kSplitBlocks * kRows * DH))[at * kRows + r] = make_float2(mx, l);
     }
   }
 }
@@ -214,55 +250,61 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
 // Joins the shares of a row: a workgroup per tile of rows
 template <int DH>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
-  __shared__ float lds_f[kMaxSplits][kRows], lds_l[kRows];
-  const int tid = threadIdx.x, group = blockIdx.x, h = group % a.c.heads, rt = group / a.c.heads % a.row_tiles, i = group / a.c.heads / a.row_tiles;
-  const Share w(a, i, rt);
+  __shared__ float lds_f[kRows][kMaxSplits], lds_l[kRows];
+  const int tid = threadIdx.x, lane = tid & 63, group = blockIdx.x;
+  const int h = group % a.c.heads, rt = group / a.c.heads % a.row_tiles, i = group / a.c.heads / a.row_tiles;
+  const Share w(a, i, rt, kWaves / parts_of(DH));
   if (rt * kRows >= w.R || w.shares == 1) return;
-  const float *part = a.part + (long)group * a.splits * kRows * (DH + 2);
-  if (tid < kRows) {  // weights of the shares
-    const float *p = part + tid * (DH + 2) + DH;
-    float mx = -__builtin_inff();
-    for (int k = 0; k < w.shares; k++) mx = fmaxf(mx, p[(long)k * kRows * (DH + 2)]);
-    const float from = mx == -__builtin_inff() ? 0.f : mx;
-    float l = 0.f;
-    for (int k = 0; k < w.shares; k++) {
-      const float f = __builtin_amdgcn_exp2f(p[(long)k * kRows * (DH + 2)] - from);
-      lds_f[k][tid] = f;
-      l += f * p[(long)k * kRows * (DH + 2) + 1];
-    }
-    lds_l[tid] = l;
+  const long at = (long)group * a.splits;
+  static_assert(kMaxSplits == 64, "a share per lane");
+  for (int r = tid >> 6; r < kRows; r += 4) {  // weights of the shares
+    const float2 ml = lane < w.shares ? ((const float2 *)(a.part + (long)kSplitBlocks * kRows * DH))[(at + lane) * kRows + r]
+                                      : make_float2(-__builtin_inff(), 0.f);
+    const float mx = wave_max(ml.x), f = __builtin_amdgcn_exp2f(ml.x - (mx == -__builtin_inff() ? 0.f : mx)), l = wave_sum(f * ml.y);
+    lds_f[r][lane] = f;
+    if (lane == 0) lds_l[r] = l;
   }
   __syncthreads();
-  for (int x = tid; x < kRows * DH; x += 256) {
-    const int r = x / DH, d = x % DH;
-    float y = 0.f;
-    for (int k = 0; k < w.shares; k++) y += lds_f[k][r] * part[((long)k * kRows + r) * (DH + 2) + d];
-    store_row(a, w, h, rt * kRows + r, d, DH, y, lds_l[r]);
+  for (int x = tid; x < kRows * DH / 4; x += 256) {
+    const int r = x / (DH / 4), d = x % (DH / 4) * 4;
+    if (rt * kRows + r >= w.R) continue;
+    const f32x4 *from = (const f32x4 *)(a.part + (at * kRows + r) * DH + d);
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int k = 0; k < w.shares; k++) y += lds_f[r][k] * from[(long)k * kRows * DH / 4];
+#pragma unroll
+    for (int k = 0; k < 4; k++) store_row(a, w, h, rt * kRows + r, d + k, DH, y[k], lds_l[r]);
   }
 }
 
-template <int DH>
-void join(const CacheAttnArgs &a, hipStream_t s) {
-  if (a.splits > 1) hipLaunchKernelGGL(cache_join_kernel<DH>, dim3((unsigned)(a.c.heads * a.row_tiles * a.r.n)), dim3(256), 0, s, a);
+template <int KIND, int DH>
+hipError_t launch(CacheAttnArgs a, long tiles, hipStream_t s) {
+  // as many workgroups as the chip holds at once, none with less than the tiles that it has in work at a time
+  const long groups = (long)a.c.heads * a.row_tiles * a.r.n, at_once = kWaves / parts_of(DH);
+  a.splits = (int)std::max<long>(1, std::min({kSplitBlocks / groups, (tiles + at_once - 1) / at_once, (long)kMaxSplits}));
+  const dim3 grid((unsigned)(groups * a.splits)), block(256);
+  if (a.r.max_new == 1) hipLaunchKernelGGL((cache_token_kernel<KIND, DH, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((cache_token_kernel<KIND, DH, false>), grid, block, 0, s, a);
+  if (a.splits > 1) hipLaunchKernelGGL(cache_join_kernel<DH>, dim3((unsigned)groups), block, 0, s, a);
+  return hipGetLastError();
 }
 
 template <int KIND>
-hipError_t launch(const CacheAttnArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)((long)a.splits * a.c.heads * a.row_tiles * a.r.n)), block(256);
+hipError_t launch_width(const CacheAttnArgs &a, long tiles, hipStream_t s) {
   switch (a.c.dh) {
-    case 64: hipLaunchKernelGGL((cache_token_kernel<KIND, 64>), grid, block, 0, s, a); join<64>(a, s); break;
-    case 128: hipLaunchKernelGGL((cache_token_kernel<KIND, 128>), grid, block, 0, s, a); join<128>(a, s); break;
-    case 256: hipLaunchKernelGGL((cache_token_kernel<KIND, 256>), grid, block, 0, s, a); join<256>(a, s); break;
-    default: hipLaunchKernelGGL((cache_token_kernel<KIND, 512>), grid, block, 0, s, a); join<512>(a, s);
+    case 64: return launch<KIND, 64>(a, tiles, s);
+    case 128: return launch<KIND, 128>(a, tiles, s);
+    case 256: return launch<KIND, 256>(a, tiles, s);
+    default: return launch<KIND, 512>(a, tiles, s);
   }
-  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_cache_token(const CacheAttnArgs &a, hipStream_t s) {
-  if (a.c.kind == CACHE_Q4) return launch<CACHE_Q4>(a, s);
-  return a.c.kind == CACHE_F16 ? launch<CACHE_F16>(a, s) : launch<CACHE_BF16>(a, s);
+hipError_t launch_cache_token(CacheAttnArgs a, long tiles, hipStream_t s) {
+  a.row_tiles = (int)(((long)a.r.max_new * a.group + kRows - 1) / kRows);
+  if (a.c.kind == CACHE_Q4) return launch_width<CACHE_Q4>(a, tiles, s);
+  return a.c.kind == CACHE_F16 ? launch_width<CACHE_F16>(a, tiles, s) : launch_width<CACHE_BF16>(a, tiles, s);
 }
 
 }  // namespace nt

@@ -30,25 +30,28 @@ __device__ __forceinline__ f16x2 q4_scale_pair(uint32_t w, int p) {
   return __builtin_bit_cast(f16x2, p == 0 ? (w & 0xFF) << 8 | (w & 0xFF00) << 16 : (w >> 8 & 0xFF00) | (w & 0xFF000000u));
 }
 
-// Keys of a tile: fragment (t, c) for the first product
-template <int KIND, int DH>
+// Keys of a tile, dims DW part .. DW part + DW - 1 of DH: fragment (t, c), c counted from there, for the first product
+template <int KIND, int DH, int DW>
 struct KeyTile {
-  static constexpr int NC = DH / 32;
-  uint4 x[KIND == CACHE_Q4 ? DH / 64 : 2 * NC];
-  uint32_t sc[KIND == CACHE_Q4 ? 2 : 1][KIND == CACHE_Q4 ? (NC + 3) / 4 : 1];
-  __device__ __forceinline__ void load(const char *tile, int lane) {
+  static constexpr int NC = DW / 32;
+  uint4 x[KIND == CACHE_Q4 ? DW / 64 : 2 * NC];
+  uint32_t sc[KIND == CACHE_Q4 ? 2 : 1];
+  __device__ __forceinline__ void load(const char *tile, int lane, int part) {
     const uint4 *p = (const uint4 *)tile + lane;
+    if constexpr (KIND != CACHE_Q4) {
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(x) / 16); i++) x[i] = p[i * 64];
-    if constexpr (KIND == CACHE_Q4) {
+      for (int t = 0; t < 2; t++)
+#pragma unroll
+        for (int c = 0; c < NC; c++) x[t * NC + c] = p[(t * (DH / 32) + part * NC + c) * 64];
+    } else {
+      static_assert(DW == 64 || DW == 128, "words of a token in one piece, or of both in one");
       const int r = lane & 15, tok = 8 * (r >> 2) + (r & 3);
 #pragma unroll
-      for (int t = 0; t < 2; t++) {
-        const char *s = tile + 32 * DH + (tok + 4 * t) * NC;
-        if constexpr (NC == 2) sc[t][0] = *(const unsigned short *)s;
-        else
+      for (int i = 0; i < DW / 64; i++) x[i] = p[(i * (DH / 128) + part) * 64];
 #pragma unroll
-          for (int i = 0; i < NC / 4; i++) sc[t][i] = ((const uint32_t *)s)[i];
+      for (int t = 0; t < 2; t++) {
+        const char *s = tile + 32 * DH + (tok + 4 * t) * (DH / 32) + part * NC;
+        sc[t] = NC == 2 ? *(const unsigned short *)s : *(const uint32_t *)s;
       }
     }
   }
@@ -59,7 +62,7 @@ struct KeyTile {
       const int w = t * NC + c;
       f16x2 v[4];
       q4_unpack(((const uint32_t *)&x[w / 4])[w % 4], v);
-      const uint32_t b = sc[t][c / 4] >> (8 * (c % 4)) & 0xFF;
+      const uint32_t b = sc[t] >> (8 * c) & 0xFF;
       const f16x2 s = __builtin_bit_cast(f16x2, b << 8 | b << 24);
 #pragma unroll
       for (int j = 0; j < 4; j++) v[j] *= s;
@@ -68,19 +71,19 @@ struct KeyTile {
   }
 };
 
-// Values of a tile: fragment n for the second product
-template <int KIND, int DH>
+// Values of a tile, the same dims: fragment n for the second product
+template <int KIND, int DH, int DW>
 struct ValueTile {
-  static constexpr int NV = DH / 16;
+  static constexpr int NV = DW / 16;
   uint4 x[KIND == CACHE_Q4 ? NV / 4 : NV];
   uint2 sc[KIND == CACHE_Q4 ? NV / 2 : 1];
-  __device__ __forceinline__ void load(const char *tile, int lane) {
-    const uint4 *p = (const uint4 *)(tile + (KIND == CACHE_Q4 ? 16 : 64) * DH) + lane;
+  __device__ __forceinline__ void load(const char *tile, int lane, int part) {
+    const uint4 *p = (const uint4 *)(tile + (KIND == CACHE_Q4 ? 16 : 64) * DH) + part * (int)(sizeof(x) / 16) * 64 + lane;
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(x) / 16); i++) x[i] = p[i * 64];
     if constexpr (KIND == CACHE_Q4) {
 #pragma unroll
-      for (int b = 0; b < NV / 2; b++) sc[b] = *(const uint2 *)(tile + 33 * DH + b * kTile + (lane >> 4) * 8);
+      for (int b = 0; b < NV / 2; b++) sc[b] = *(const uint2 *)(tile + 33 * DH + (part * (NV / 2) + b) * kTile + (lane >> 4) * 8);
     }
   }
   // Values of this lane's eight tokens that are no query's become zero, whatever they are: bit j of `keep` stays
