@@ -78,12 +78,15 @@ struct CacheAttnArgs {
   float scale;
   int32_t window, sinks;
   int32_t vec, vec_out;  // query rows, output rows are 16-byte aligned
-  float *part;           // kSplitBlocks x 8 x (dh + 2)
-  // set by the launchers: tiles of query rows of a sequence, workgroups that share their keys
-  int32_t row_tiles, splits;
+  float *part;           // [share][row][dh], behind them {maximum, sum} [share][row]
+  long part_floats;
+  // set by the launchers: tiles of query rows of a sequence, workgroups that share their keys, tiles of keys that each has at
+  // least, rows of a share
+  int32_t row_tiles, splits, least, part_rows;
+  float2 *part_sums;
 };
-constexpr int kSplitBlocks = 1024;  // workgroups among which split keys are spread, at most
-constexpr int kMaxSplits = 64;      // of one row: a workgroup of the join reads them all
+constexpr int kMaxSplits = 64;  // shares of one row's keys: a lane each in the join
+constexpr long kPartFloats = 8l << 20;  // what the shares of a call leave for the join, at most: 16,000 of 4 rows of 128
 // Queries in tiles of 8 (rows: token, then head of the group), each split over the keys, of which a row sees about `tiles` tiles.
 hipError_t launch_cache_token(CacheAttnArgs a, long tiles, hipStream_t s);
 // Tiles of 128 to 256 query rows, unsplit.

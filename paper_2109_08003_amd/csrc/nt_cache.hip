@@ -654,6 +654,7 @@ struct nt_cache {
   int device = -1;
   char *mem = nullptr;
   float *part = nullptr;
+  long part_floats = 0;
   int32_t *h_flags = nullptr;  // pinned
 };
 
@@ -716,7 +717,9 @@ size_t lay_out(nt_cache *c, char *base) {
   v.ref = ints(g.n_pages); v.used = (uint32_t *)ints((g.n_pages + 31) / 32); v.flags = ints(2);
   c->w.off = ints(g.max_seqs); c->w.list = ints(g.n_pages); c->w.from = ints(g.n_pages); c->w.to = ints(g.n_pages);
   c->w.info = ints(2); c->w.row_len = ints(g.max_seqs); c->w.row = ints((size_t)g.max_seqs * v.width);
-  c->part = (float *)take((size_t)nt::kSplitBlocks * 8 * (g.d_head + 2) * 4);
+  // for the most shares that single tokens of all sequences can have
+  c->part_floats = (long)std::min<double>(nt::kPartFloats, (double)g.max_seqs * g.n_q_heads * nt::kMaxSplits * (g.d_head + 2)) & ~3l;
+  c->part = (float *)take((size_t)c->part_floats * 4);
   return off;
 }
 
@@ -956,7 +959,7 @@ hipError_t nt::cache_attend(nt_cache *c, const nt_attend_args &a, int out_type, 
   k.layer = a.layer; k.type = a.type; k.out_type = out_type; k.q_heads = g.n_q_heads; k.group = g.n_q_heads / g.n_kv_heads;
   k.q = a.q; k.out = a.out; k.ld_q = a.ld_q; k.ld_out = a.ld_out; k.lo_offset = lo_offset;
   k.scale = a.scale; k.window = a.window; k.sinks = a.sinks; k.vec = aligned(a.q, a.ld_q, a.type); k.vec_out = aligned(a.out, a.ld_out, a.type);
-  k.part = c->part;
+  k.part = c->part; k.part_floats = c->part_floats;
   if ((long)a.max_new * k.group > 64) return launch_cache_prompt(k, s);
   long keys = a.max_keys > 0 ? std::min(a.max_keys, g.max_len) : g.max_len;
   if (a.window > 0) keys = std::min<long>(keys, (long)a.window + a.sinks + a.max_new + 2 * kTile);

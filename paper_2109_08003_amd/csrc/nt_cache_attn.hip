@@ -7,13 +7,14 @@
 // products have twice the bits at no cost: reading the keys and values is what such a call is bound by.
 // The waves meet in the LDS; where several workgroups share the keys of a row, a second launch joins what they left in memory.
 #include <algorithm>
+#include <climits>
 
 #include "nt_cache_frag.h"
 
 namespace nt {
 namespace {
 
-constexpr int kRows = 8, kWaves = 4;
+constexpr int kRows = 8, kWaves = 4, kFill = 1024;
 // Waves that share a tile, 128 dims each, and so tiles in work at a time: beyond 128 dims the accumulators, keys and values of a
 // wave would leave one wave to a SIMD.  Their parts of the scores are added through the LDS.
 constexpr int parts_of(int dh) { return dh > 128 ? dh / 128 : 1; }
@@ -26,7 +27,7 @@ struct Share {
   int first, p_min, p_max, low;            // positions: of the first new token, of the rows; first key of the earliest window
   int sink_tiles, window_tile, tiles, per, shares;
   bool known;
-  __device__ __forceinline__ Share(const CacheAttnArgs &a, int i, int rt, int at_once) {
+  __device__ __forceinline__ Share(const CacheAttnArgs &a, int i, int rt) {
     s = a.r.seq ? a.r.seq[i] : i;
     row0 = a.r.first ? a.r.first[i] : i;
     m = a.r.first ? a.r.first[i + 1] - (int)row0 : 1;
@@ -40,7 +41,7 @@ struct Share {
     sink_tiles = (min(a.sinks, low) + kTile - 1) / kTile;
     window_tile = max(low / kTile, sink_tiles);
     tiles = p_max < 0 ? 0 : sink_tiles + max(p_max / kTile + 1 - window_tile, 0);
-    per = max((tiles + a.splits - 1) / a.splits, at_once);
+    per = max((tiles + a.splits - 1) / a.splits, a.least);
     shares = max((tiles + per - 1) / per, 1);
   }
 };
@@ -53,7 +54,7 @@ __device__ __forceinline__ void store_row(const CacheAttnArgs &a, const Share &w
 
 // ONE: every sequence has one new token, so the rows of a workgroup see the same keys
 template <int KIND, int DH, bool ONE>
-__global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
+__global__ __launch_bounds__(256, (ONE ? 2 : 1)) void cache_token_kernel(CacheAttnArgs a) {
   typedef typename FragType<KIND>::type F;
   typedef typename FragType<KIND>::elem E;
   constexpr int PARTS = parts_of(DH), GROUPS = kWaves / PARTS, DW = DH / PARTS, NC = DW / 32, NV = DW / 16;
@@ -63,11 +64,11 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
   char *lds_q = (char *)lds_o;  // before the loop
   static_assert(sizeof(lds_o) >= DH * 32, "");
   const CacheView &c = a.c;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g4 = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g4 = lane >> 4;
   const int part = wave % PARTS, mine = wave / PARTS;  // of a tile's dims, of the tiles in work
   const int split = blockIdx.x % a.splits, group = blockIdx.x / a.splits, h = group % c.heads, rt = group / c.heads % a.row_tiles,
             i = group / c.heads / a.row_tiles;
-  const Share w(a, i, rt, GROUPS);
+  const Share w(a, i, rt);
   const int G = a.group;
   if ((!w.known || w.m < 0 || w.m > a.r.max_new || w.m > w.len) && split == 0 && h == 0 && rt == 0 && tid == 0) atomicOr(c.flags, 1);
   if (rt * kRows >= w.R || split >= w.shares) return;
@@ -84,8 +85,8 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
 #pragma unroll
     for (int k = 1; k < DH / 8; k *= 2) big = fmaxf(big, __shfl_xor(big, k, 64));
     const int e = big > 0.f && big < __builtin_inff() ? min(max(ilogbf(big), -100), 126) : 0;
-    if (d == 0) lds_scale[r] = ldexpf(a.scale * 1.44269504088896f, e);
-    const float down = ldexpf(1.f, -e);
+    if (d == 0) lds_scale[r] = ldexpf(fabsf(a.scale) * 1.44269504088896f, e);
+    const float down = ldexpf(a.scale < 0.f ? -1.f : 1.f, -e);
     F head, tail;
 #pragma unroll
     for (int k = 0; k < 8; k++) {
@@ -126,7 +127,7 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
   f32x4 o[NV];
 #pragma unroll
   for (int n = 0; n < NV; n++) o[n] = zero;
-  float top = -__builtin_inff(), sum = 0.f;
+  float top = kLowest, sum = 0.f;
   int turn = 0;
   for (; PARTS > 1 ? t - mine < t1 : t < t1; t += GROUPS) {  // waves that meet make the same number of turns
     const int j0 = tile_of(t) * kTile;
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
 #pragma unroll
     for (int j = 0; j < 8; j++) {
       const float x = sc[j / 4][j % 4];
-      y[j] = (x + __uint_as_float(wave_dpp<0x128>(__float_as_uint(x)))) * to_log2;  // head and tail: columns 8 apart
+      y[j] = x + __uint_as_float(wave_dpp<0x128>(__float_as_uint(x)));  // head and tail: columns 8 apart
     }
     const bool all_seen =
         page >= 0 && j0 + kTile - 1 <= w.p_min && (a.window == 0 || j0 >= w.p_max - a.window + 1 || j0 + kTile <= a.sinks);
@@ -175,25 +176,37 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
       }
       vt.clear(someone);
     }
-    float tile_top = y[0];
+    float z[8];
+    auto weigh = [&]() {
+      int big = INT_MIN;
 #pragma unroll
-    for (int j = 1; j < 8; j++) tile_top = fmaxf(tile_top, y[j]);
-    tile_top = wave_pair16(tile_top, tile_top, WaveMax{});
-    tile_top = wave_pair32(tile_top, tile_top, WaveMax{});
-    const float up = fmaxf(top, tile_top), from = up == -__builtin_inff() ? 0.f : up;
-    const float shrink = __builtin_amdgcn_exp2f(top - from);
-    top = up;
-    sum *= shrink;
+      for (int j = 0; j < 8; j++) {
+        z[j] = __builtin_fmaf(y[j], to_log2, -top);
+        big = max(big, __float_as_int(z[j]));  // of positive numbers the largest
+      }
+      return big;
+    };
+    if (__any(weigh() > __float_as_int(kSlack))) {  // some row: those that need it change their maximum, no other row depends on them
+      float mx = y[0];
+#pragma unroll
+      for (int j = 1; j < 8; j++) mx = fmaxf(mx, y[j]);
+      mx = wave_pair16(mx, mx, WaveMax{});
+      mx = wave_pair32(mx, mx, WaveMax{}) * to_log2;
+      const float up = mx - top > kSlack ? mx : top, shrink = __builtin_amdgcn_exp2f(top - up);
+      top = up;
+      sum *= shrink;
+#pragma unroll
+      for (int n = 0; n < NV; n++) o[n] *= shrink;
+      weigh();
+    }
     F p;
 #pragma unroll
     for (int j = 0; j < 8; j++) {
-      const float x = __builtin_amdgcn_exp2f(y[j] - from);
+      const float x = __builtin_amdgcn_exp2f(z[j]);
       sum += x;
       const E head = (E)x;
       p[j] = col < 8 ? head : (E)(x - (float)head);
     }
-#pragma unroll
-    for (int n = 0; n < NV; n++) o[n] *= shrink;
     bool bad = false;
     if (!ONE && !all_seen && w.p_min < w.p_max) {  // rows of different tokens: some see keys that others do not
 #pragma unroll
@@ -213,7 +226,7 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
   sum = wave_pair16(sum, sum, WaveAdd{});
   sum = wave_pair32(sum, sum, WaveAdd{});
 
-  const long at = (long)group * a.splits + split;  // [workgroup][row][dim], then [workgroup][row] {maximum, sum}
+  const long at = ((long)group * a.splits + split) * a.part_rows;
   __syncthreads();                                 // the last use of the LDS
   if (lane < 8 && part == 0) lds_m[mine][lane] = top, lds_l[mine][lane] = sum;
 #pragma unroll
@@ -230,19 +243,18 @@ __global__ __launch_bounds__(256) void cache_token_kernel(CacheAttnArgs a) {
     float mx = lds_m[0][r];
 #pragma unroll
     for (int k = 1; k < GROUPS; k++) mx = fmaxf(mx, lds_m[k][r]);
-    const float from = mx == -__builtin_inff() ? 0.f : mx;
     float l = 0.f, y = 0.f;
 #pragma unroll
     for (int k = 0; k < GROUPS; k++) {
-      const float f = __builtin_amdgcn_exp2f(lds_m[k][r] - from);
+      const float f = __builtin_amdgcn_exp2f(lds_m[k][r] - mx);
       l += f * lds_l[k][r];
       y += f * lds_o[k][r][d];
     }
     if (w.shares == 1) {
       store_row(a, w, h, rt * kRows + r, d, DH, y, l);
     } else {
-      a.part[(at * kRows + r) * DH + d] = y;
-      if (d == 0) ((float2 *)(a.part + (long)kSplitBlocks * kRows * DH))[at * kRows + r] = make_float2(mx, l);
+      a.part[(at + r) * DH + d] = y;
+      if (d == 0) a.part_sums[at + r] = make_float2(mx, l);
     }
   }
 }
@@ -253,25 +265,24 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
   __shared__ float lds_f[kRows][kMaxSplits], lds_l[kRows];
   const int tid = threadIdx.x, lane = tid & 63, group = blockIdx.x;
   const int h = group % a.c.heads, rt = group / a.c.heads % a.row_tiles, i = group / a.c.heads / a.row_tiles;
-  const Share w(a, i, rt, kWaves / parts_of(DH));
+  const Share w(a, i, rt);
   if (rt * kRows >= w.R || w.shares == 1) return;
-  const long at = (long)group * a.splits;
+  const long at = (long)group * a.splits * a.part_rows;
   static_assert(kMaxSplits == 64, "a share per lane");
-  for (int r = tid >> 6; r < kRows; r += 4) {  // weights of the shares
-    const float2 ml = lane < w.shares ? ((const float2 *)(a.part + (long)kSplitBlocks * kRows * DH))[(at + lane) * kRows + r]
-                                      : make_float2(-__builtin_inff(), 0.f);
-    const float mx = wave_max(ml.x), f = __builtin_amdgcn_exp2f(ml.x - (mx == -__builtin_inff() ? 0.f : mx)), l = wave_sum(f * ml.y);
+  const int rows = min(w.R - rt * kRows, kRows);
+  for (int r = tid >> 6; r < rows; r += 4) {  // weights of the shares
+    const float2 ml = lane < w.shares ? a.part_sums[at + lane * a.part_rows + r] : make_float2(kLowest, 0.f);
+    const float mx = wave_max(ml.x), f = __builtin_amdgcn_exp2f(ml.x - mx), l = wave_sum(f * ml.y);
     lds_f[r][lane] = f;
     if (lane == 0) lds_l[r] = l;
   }
   __syncthreads();
-  for (int x = tid; x < kRows * DH / 4; x += 256) {
+  for (int x = tid; x < rows * DH / 4; x += 256) {
     const int r = x / (DH / 4), d = x % (DH / 4) * 4;
-    if (rt * kRows + r >= w.R) continue;
-    const f32x4 *from = (const f32x4 *)(a.part + (at * kRows + r) * DH + d);
+    const f32x4 *from = (const f32x4 *)(a.part + (at + r) * DH + d);
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-    for (int k = 0; k < w.shares; k++) y += lds_f[r][k] * from[(long)k * kRows * DH / 4];
+    for (int k = 0; k < w.shares; k++) y += lds_f[r][k] * from[(long)k * a.part_rows * DH / 4];
 #pragma unroll
     for (int k = 0; k < 4; k++) store_row(a, w, h, rt * kRows + r, d + k, DH, y[k], lds_l[r]);
   }
@@ -279,9 +290,17 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
 
 template <int KIND, int DH>
 hipError_t launch(CacheAttnArgs a, long tiles, hipStream_t s) {
-  // as many workgroups as the chip holds at once, none with less than the tiles that it has in work at a time
+  // Shares of the keys.  Up to 1,024 workgroups, four to a CU, as many as have a turn each; beyond that as many as have kTurns, so that
+  // the longest sequences do not run on when the others are done: 64 sequences of 500 to 16,000 tokens, 8 heads, 235 us with
+  // two shares and 218 with 15; 256 in 4 bits 391 with one and 291 with 7.  Turns 2 / 4 / 8 / 16: 225 / 220 / 218 / 221, 304 / 300 / 291 / 283.
+  constexpr int kTurns = 8;
   const long groups = (long)a.c.heads * a.row_tiles * a.r.n, at_once = kWaves / parts_of(DH);
-  a.splits = (int)std::max<long>(1, std::min({kSplitBlocks / groups, (tiles + at_once - 1) / at_once, (long)kMaxSplits}));
+  a.part_rows = (int)std::min<long>(kRows, (long)a.r.max_new * a.group);
+  const long slots = a.part_floats / (a.part_rows * (DH + 2)), turns = (tiles + at_once - 1) / at_once;
+  const long few = std::min(kFill / groups, turns), many = std::min(slots / groups, turns / kTurns);
+  a.splits = (int)std::max<long>(1, std::min<long>(std::max(few, many), std::min<long>(kMaxSplits, slots / groups)));
+  a.least = (int)(at_once * (few >= many ? 1 : kTurns));
+  a.part_sums = (float2 *)(a.part + slots * a.part_rows * DH);
   const dim3 grid((unsigned)(groups * a.splits)), block(256);
   if (a.r.max_new == 1) hipLaunchKernelGGL((cache_token_kernel<KIND, DH, true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((cache_token_kernel<KIND, DH, false>), grid, block, 0, s, a);

@@ -5,6 +5,11 @@
 
 namespace nt {
 
+// The running maximum of a row changes only where a score exceeds it by more than kSlack (as a logarithm of base 2): weights are up to
+// 2^8 then, which no type here minds, and most tiles rescale nothing.
+constexpr float kSlack = 8.f;
+constexpr float kLowest = -1e38f;  // maximum of no score; less than any that is a number
+
 template <int KIND> struct FragType { typedef f16x8 type; typedef _Float16 elem; };
 template <> struct FragType<CACHE_BF16> { typedef bf16x8 type; typedef __bf16 elem; };
 
@@ -25,9 +30,10 @@ __device__ __forceinline__ f16x8 q4_join(const f16x2 (&x)[4]) {
   for (int j = 0; j < 8; j++) r[j] = x[j / 2][j % 2];
   return r;
 }
-// two scale bytes (at bit positions 16 p and 16 p + 8 of w) as fp16 numbers
-__device__ __forceinline__ f16x2 q4_scale_pair(uint32_t w, int p) {
-  return __builtin_bit_cast(f16x2, p == 0 ? (w & 0xFF) << 8 | (w & 0xFF00) << 16 : (w >> 8 & 0xFF00) | (w & 0xFF000000u));
+// scale bytes i and j of w as fp16 numbers
+template <int I, int J>
+__device__ __forceinline__ f16x2 q4_scales(uint32_t w) {
+  return __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(w, w, 0x000C000Cu | I << 8 | (uint32_t)J << 24));  // selector 12: a zero byte
 }
 
 // Keys of a tile, dims DW part .. DW part + DW - 1 of DH: fragment (t, c), c counted from there, for the first product
@@ -62,8 +68,7 @@ struct KeyTile {
       const int w = t * NC + c;
       f16x2 v[4];
       q4_unpack(((const uint32_t *)&x[w / 4])[w % 4], v);
-      const uint32_t b = sc[t] >> (8 * c) & 0xFF;
-      const f16x2 s = __builtin_bit_cast(f16x2, b << 8 | b << 24);
+      const f16x2 s = c == 0 ? q4_scales<0, 0>(sc[t]) : c == 1 ? q4_scales<1, 1>(sc[t]) : c == 2 ? q4_scales<2, 2>(sc[t]) : q4_scales<3, 3>(sc[t]);
 #pragma unroll
       for (int j = 0; j < 4; j++) v[j] *= s;
       return q4_join(v);
@@ -107,10 +112,10 @@ struct ValueTile {
     } else {
       f16x2 v[4];
       q4_unpack(((const uint32_t *)&x[n / 4])[n % 4], v);
-      v[0] *= q4_scale_pair(sc[n / 2].x, 0);
-      v[1] *= q4_scale_pair(sc[n / 2].x, 1);
-      v[2] *= q4_scale_pair(sc[n / 2].y, 0);
-      v[3] *= q4_scale_pair(sc[n / 2].y, 1);
+      v[0] *= q4_scales<0, 1>(sc[n / 2].x);
+      v[1] *= q4_scales<2, 3>(sc[n / 2].x);
+      v[2] *= q4_scales<0, 1>(sc[n / 2].y);
+      v[3] *= q4_scales<2, 3>(sc[n / 2].y);
       return q4_join(v);
     }
   }

@@ -30,9 +30,6 @@ __device__ __forceinline__ uint32_t no_numbers(uint32_t w) {
   return (b << 1) - (b >> 15);
 }
 
-constexpr float kSlack = 8.f;     // log2 by which a weight may exceed 1 before sums and accumulators are rescaled
-constexpr float kLowest = -1e38f;  // maximum of no score; less than any that is a number
-
 template <int KIND, int DH>
 __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_kernel(CacheAttnArgs a, int spread) {
   typedef typename FragType<KIND>::type F;
@@ -166,13 +163,13 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
           f16x2 v[4];
           q4_unpack(((const uint32_t *)&code[y])[w], v);
           if (p < PIECES / 2) {
-            const uint32_t by = (NC == 2 ? sc[y][w / 2] >> (8 * (w % 2)) : sc[y][0] >> (8 * w)) & 0xFF;
-            const f16x2 f = __builtin_bit_cast(f16x2, by << 8 | by << 24);
+            const uint32_t by = NC == 2 ? sc[y][w / 2] >> (8 * (w % 2)) : sc[y][0] >> (8 * w);
+            const f16x2 f = q4_scales<0, 0>(by);
 #pragma unroll
             for (int d = 0; d < 4; d++) v[d] *= f;
           } else {
 #pragma unroll
-            for (int d = 0; d < 4; d++) v[d] *= q4_scale_pair(sc[y][w / 2 * 2 + d / 2], d % 2);
+            for (int d = 0; d < 4; d++) v[d] *= d % 2 ? q4_scales<2, 3>(sc[y][w / 2 * 2 + d / 2]) : q4_scales<0, 1>(sc[y][w / 2 * 2 + d / 2]);
           }
           *(f16x8 *)(to + w * 1024) = q4_join(v);
         }
