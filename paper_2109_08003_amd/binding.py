@@ -385,6 +385,12 @@ class Cache:
         h = C.c_void_p()
         _check(lib().nt_cache_create(C.byref(self.config), _stream_ptr(stream), C.byref(h)))
         self._h = h
+        # what every call needs, looked up once: a step of a few sequences is a call of a few microseconds
+        import torch
+        self._lib, self._int32, self._types = lib(), torch.int32, {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+        self._current_stream, self._scale = torch.cuda.current_stream, d_head ** -0.5
+        self._args = NtAttendArgs(C.sizeof(NtAttendArgs))
+        self._args_ref = C.byref(self._args)
 
     @staticmethod
     def _make_config(kind, n_layers, n_q_heads, n_kv_heads, d_head, n_pages, max_seqs, max_len, page_tokens=64) -> NtCacheConfig:
@@ -397,6 +403,9 @@ class Cache:
         c = cls._make_config(*args, **kw)
         return int(lib().nt_cache_bytes(C.byref(c)))
 
+    def _stream(self, stream) -> int:
+        return (self._current_stream() if stream is None else stream).cuda_stream
+
     def close(self):
         if getattr(self, "_h", None):
             lib().nt_cache_destroy(self._h)
@@ -408,28 +417,29 @@ class Cache:
         except Exception:
             pass
 
-    def _type(self, *tensors) -> int:
-        import torch
-        types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
-        if any(t.dtype is not tensors[0].dtype for t in tensors) or tensors[0].dtype not in types:
-            raise TypeError("tensors of one type, float32, float16 or bfloat16, are needed")
-        return types[tensors[0].dtype]
+    def _type(self, t, *others) -> int:
+        dtype = t.dtype
+        for o in others:
+            if o.dtype is not dtype:
+                raise TypeError("tensors of one type are needed")
+        try:
+            return self._types[dtype]
+        except KeyError:
+            raise TypeError("float32, float16 or bfloat16 is needed") from None
 
-    @staticmethod
-    def _ints(t, size):
-        import torch
+    def _ints(self, t, size):
         if t is None:
             return None
-        if t.dtype is not torch.int32 or not t.is_cuda or not t.is_contiguous() or t.numel() < size:
+        if t.dtype is not self._int32 or not t.is_cuda or not t.is_contiguous() or t.numel() < size:
             raise TypeError(f"a contiguous int32 cuda tensor of at least {size} entries is needed")
         return t.data_ptr()
 
     def _rows(self, t, heads):
-        """Row stride of a [rows, heads, d_head] tensor whose heads are dense."""
-        d = self.config.d_head
-        if not t.is_cuda or t.dim() != 3 or tuple(t.shape[1:]) != (heads, d) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+        """(rows, row stride) of a [rows, heads, d_head] tensor whose heads are dense."""
+        d, shape, stride = self.config.d_head, t.shape, t.stride()
+        if len(shape) != 3 or shape[1] != heads or shape[2] != d or stride[2] != 1 or (heads > 1 and stride[1] != d) or not t.is_cuda:
             raise TypeError(f"a cuda tensor [rows, {heads}, {d}] with dense heads is needed")
-        return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * d)
+        return shape[0], stride[0] if shape[0] > 1 else max(stride[0], heads * d)
 
     def _count(self, n, seqs):
         if n is None and seqs is None:
@@ -438,72 +448,77 @@ class Cache:
 
     def reserve(self, n: int = None, seqs=None, first=None, stream=None):
         n = self._count(n, seqs)
-        _check(lib().nt_cache_reserve(self._h, n, self._ints(seqs, n), self._ints(first, n + 1), _stream_ptr(stream)))
+        _check(self._lib.nt_cache_reserve(self._h, n, self._ints(seqs, n), self._ints(first, n + 1), self._stream(stream)))
 
     def write(self, k, v, n: int = None, seqs=None, first=None, max_new: int = 1, layer: int = 0, stream=None):
         n, heads = self._count(n, seqs), self.config.n_kv_heads
-        ld = self._rows(k, heads)
-        if self._rows(v, heads) != ld or k.shape != v.shape:
+        rows, ld = self._rows(k, heads)
+        if self._rows(v, heads) != (rows, ld):
             raise TypeError("k and v need the same shape and strides")
-        if first is None and k.shape[0] < n:
+        if first is None and rows < n:
             raise TypeError(f"{n} rows are needed")
-        _check(lib().nt_cache_write(self._h, layer, n, self._ints(seqs, n), self._ints(first, n + 1), max_new, k.data_ptr(), v.data_ptr(), ld,
-                                    self._type(k, v), _stream_ptr(stream)))
+        _check(self._lib.nt_cache_write(self._h, layer, n, self._ints(seqs, n), self._ints(first, n + 1), max_new, k.data_ptr(), v.data_ptr(), ld,
+                                        self._type(k, v), self._stream(stream)))
 
     def attend(self, q, out, n: int = None, seqs=None, first=None, k=None, v=None, max_new: int = 1, max_keys: int = 0, window: int = 0,
                sinks: int = 0, scale: float = None, layer: int = 0, stream=None):
-        n, g = self._count(n, seqs), self.config
-        a = NtAttendArgs(C.sizeof(NtAttendArgs), layer, n, max_new, max_keys, 0, window, sinks, g.d_head ** -0.5 if scale is None else scale)
-        a.d_seq, a.d_first = self._ints(seqs, n), self._ints(first, n + 1)
-        a.q, a.out, a.ld_q, a.ld_out = q.data_ptr(), out.data_ptr(), self._rows(q, g.n_q_heads), self._rows(out, g.n_q_heads)
-        tensors = [q, out]
-        if out.shape != q.shape:
+        n, g, a = self._count(n, seqs), self.config, self._args
+        rows, a.ld_q = self._rows(q, g.n_q_heads)
+        rows_out, a.ld_out = self._rows(out, g.n_q_heads)
+        if rows_out != rows:
             raise TypeError("q and out need the same shape")
         if k is not None or v is not None:
-            if k is None or v is None or k.shape != v.shape or k.shape[0] != q.shape[0] or self._rows(k, g.n_kv_heads) != self._rows(v, g.n_kv_heads):
+            if k is None or v is None:
+                raise TypeError("k and v go together")
+            rows_k, a.ld_kv = self._rows(k, g.n_kv_heads)
+            if rows_k != rows or self._rows(v, g.n_kv_heads) != (rows_k, a.ld_kv):
                 raise TypeError("k and v need q's rows, and the same shape and strides")
-            a.k, a.v, a.ld_kv = k.data_ptr(), v.data_ptr(), self._rows(k, g.n_kv_heads)
-            tensors += [k, v]
-        if first is None and q.shape[0] < n:
+            a.k, a.v, a.type = k.data_ptr(), v.data_ptr(), self._type(q, out, k, v)
+        else:
+            a.k, a.v, a.type = None, None, self._type(q, out)
+        if first is None and rows < n:
             raise TypeError(f"{n} rows are needed")
-        a.type = self._type(*tensors)
-        _check(lib().nt_cache_attend(self._h, C.byref(a), _stream_ptr(stream)))
+        a.layer, a.n, a.max_new, a.max_keys, a.window, a.sinks = layer, n, max_new, max_keys, window, sinks
+        a.scale = self._scale if scale is None else scale
+        a.d_seq, a.d_first, a.q, a.out = self._ints(seqs, n), self._ints(first, n + 1), q.data_ptr(), out.data_ptr()
+        _check(self._lib.nt_cache_attend(self._h, self._args_ref, self._stream(stream)))
 
     def read(self, k, v, n: int = None, seqs=None, layer: int = 0, stream=None):
         """k, v [n, max_keys, n_kv_heads, d_head], dense."""
         n, g = self._count(n, seqs), self.config
-        if k.shape != v.shape or k.dim() != 4 or k.shape[0] < n or tuple(k.shape[2:]) != (g.n_kv_heads, g.d_head) or not (
+        shape = k.shape
+        if v.shape != shape or len(shape) != 4 or shape[0] < n or shape[2] != g.n_kv_heads or shape[3] != g.d_head or not (
                 k.is_cuda and v.is_cuda and k.is_contiguous() and v.is_contiguous()):
             raise TypeError(f"contiguous cuda tensors [{n}, max_keys, {g.n_kv_heads}, {g.d_head}] are needed")
-        _check(lib().nt_cache_read(self._h, layer, n, self._ints(seqs, n), k.shape[1], k.data_ptr(), v.data_ptr(), self._type(k, v),
-                                   _stream_ptr(stream)))
+        _check(self._lib.nt_cache_read(self._h, layer, n, self._ints(seqs, n), shape[1], k.data_ptr(), v.data_ptr(), self._type(k, v),
+                                   self._stream(stream)))
 
     def fork(self, src, dst, stream=None):
         n = src.numel()
-        _check(lib().nt_cache_fork(self._h, n, self._ints(src, n), self._ints(dst, n), _stream_ptr(stream)))
+        _check(self._lib.nt_cache_fork(self._h, n, self._ints(src, n), self._ints(dst, n), self._stream(stream)))
 
     def copy(self, src, dst, stream=None):
         n = src.numel()
-        _check(lib().nt_cache_copy(self._h, n, self._ints(src, n), self._ints(dst, n), _stream_ptr(stream)))
+        _check(self._lib.nt_cache_copy(self._h, n, self._ints(src, n), self._ints(dst, n), self._stream(stream)))
 
     def truncate(self, n: int = None, seqs=None, lengths=None, stream=None):
         """Cut sequences back to these lengths; None ends them."""
         n = self._count(n, seqs)
-        _check(lib().nt_cache_truncate(self._h, n, self._ints(seqs, n), self._ints(lengths, n), _stream_ptr(stream)))
+        _check(self._lib.nt_cache_truncate(self._h, n, self._ints(seqs, n), self._ints(lengths, n), self._stream(stream)))
 
     def trim(self, window: int, sinks: int = 0, n: int = None, seqs=None, stream=None):
         n = self._count(n, seqs)
-        _check(lib().nt_cache_trim(self._h, n, self._ints(seqs, n), window, sinks, _stream_ptr(stream)))
+        _check(self._lib.nt_cache_trim(self._h, n, self._ints(seqs, n), window, sinks, self._stream(stream)))
 
     def compact(self, stream=None):
-        _check(lib().nt_cache_compact(self._h, _stream_ptr(stream)))
+        _check(self._lib.nt_cache_compact(self._h, self._stream(stream)))
 
     def lengths(self, stream=None):
         """(lengths int32 [max_seqs], pages int32 [2]: in use, and the last one in use plus one), cuda tensors."""
         import torch
         n, p = (torch.empty(k, dtype=torch.int32, device="cuda") for k in (self.config.max_seqs, 2))
-        _check(lib().nt_cache_lengths(self._h, n.data_ptr(), p.data_ptr(), _stream_ptr(stream)))
+        _check(self._lib.nt_cache_lengths(self._h, n.data_ptr(), p.data_ptr(), self._stream(stream)))
         return n, p
 
     def check(self, stream=None):
-        _check(lib().nt_cache_check(self._h, _stream_ptr(stream)))
+        _check(self._lib.nt_cache_check(self._h, self._stream(stream)))

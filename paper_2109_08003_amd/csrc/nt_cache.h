@@ -65,6 +65,7 @@ struct CacheReadArgs {
   CacheRows r;
   int32_t layer, type, max_keys, tiles;
   void *k, *v;
+  int32_t vec;  // 16-byte aligned
 };
 hipError_t launch_cache_read(const CacheReadArgs &a, hipStream_t s);
 

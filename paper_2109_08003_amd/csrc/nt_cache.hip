@@ -6,6 +6,7 @@
 // left - rows of the page table, counts of holders, contents of pages - is done by launches over the whole chip.
 #include <algorithm>
 #include <climits>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <new>
@@ -187,24 +188,29 @@ __global__ __launch_bounds__(kPlan) void cache_reserve_kernel(CacheView c, Cache
 // ---- contents of pages -----------------------------------------------------------------------------------------------
 
 constexpr int kCopyPiece = 16384;  // bytes a workgroup of 256 copies at a time: four loads in flight per thread
-// Copies the pages of from[] to to[] in all layers; this is workgroup `block` of `blocks`.
+__host__ __device__ inline int copy_pieces(const CacheView &c) { return (int)((c.page_bytes + kCopyPiece - 1) / kCopyPiece); }
+// Copies the pages of from[] to to[] in all layers; this is workgroup `block` of `blocks`, a multiple of layers x pieces.
 __device__ void copy_pages(const CacheView &c, int layers, const PageWork &w, int block, int blocks) {
-  const long pieces = (c.page_bytes + kCopyPiece - 1) / kCopyPiece, all = (long)w.info[0] * layers * pieces;
-  for (long t = block; t < all; t += blocks) {
-    const long piece = t % pieces, l = t / pieces % layers, k = t / pieces / layers;
-    const long at = piece * kCopyPiece + threadIdx.x * 16;
-    const char *src = c.pool + l * c.layer_bytes + w.from[k] * c.page_bytes + at;
-    char *dst = c.pool + l * c.layer_bytes + w.to[k] * c.page_bytes + at;
-    uint4 x[kCopyPiece / 4096];
-#pragma unroll
-    for (int j = 0; j < kCopyPiece / 4096; j++)
-      if (at + j * 4096 < c.page_bytes) x[j] = *(const uint4 *)(src + j * 4096);
-#pragma unroll
-    for (int j = 0; j < kCopyPiece / 4096; j++)
-      if (at + j * 4096 < c.page_bytes) *(uint4 *)(dst + j * 4096) = x[j];
+  const int pieces = copy_pieces(c), each = pieces * layers, piece = block % pieces, l = block / pieces % layers;
+  const long at = (long)piece * kCopyPiece + threadIdx.x * 16;
+  char *base = c.pool + l * c.layer_bytes + at;
+  const int copies = w.info[0];
+  for (int k = block / each; k < copies; k += blocks / each) {
+    const char *src = base + w.from[k] * c.page_bytes;
+    char *dst = base + w.to[k] * c.page_bytes;
+    if ((long)(piece + 1) * kCopyPiece <= c.page_bytes) {
+      const uint4 x0 = *(const uint4 *)src, x1 = *(const uint4 *)(src + 4096), x2 = *(const uint4 *)(src + 8192), x3 = *(const uint4 *)(src + 12288);
+      *(uint4 *)dst = x0, *(uint4 *)(dst + 4096) = x1, *(uint4 *)(dst + 8192) = x2, *(uint4 *)(dst + 12288) = x3;
+    } else {
+      for (int j = 0; at + j < c.page_bytes; j += 4096) *(uint4 *)(dst + j) = *(const uint4 *)(src + j);
+    }
   }
 }
-constexpr int kCopyBlocks = 2048;
+// Workgroups for copies of at most `pages` pages
+int copy_blocks(const CacheView &c, int layers, double pages) {
+  const int each = copy_pieces(c) * layers;
+  return each * (int)std::max(1.0, std::min(pages, std::ceil(2048.0 / each)));
+}
 
 // ---- sequences that become others -------------------------------------------------------------------------------------
 
@@ -218,20 +224,66 @@ __device__ __forceinline__ int copies_of(const CacheView &c, int src, bool deep,
   return wave_fold(n, WaveAdd{});
 }
 
-__global__ __launch_bounds__(kPlan) void cache_fork_plan_kernel(CacheView c, int n, const int32_t *src, const int32_t *dst, int deep, PageWork w) {
+// Entry i, by `lanes` lanes of a wave, of which this is number `lane`: the source's row as the target will have it, holders of
+// shared pages, pages to be copied
+__device__ void fork_stage(const CacheView &c, int i, int src, bool deep, const PageWork &w, int lane, int lanes) {
+  const int shift = (threadIdx.x & 63) - lane;
+  const unsigned long long before = (1ull << lane) - 1, all = lanes == 64 ? ~0ull : (1ull << lanes) - 1;
+  int at = w.off[i];
+  if (at < 0) return;
+  const int len = c.len[src], np = pages_of(c, len), full = len >> c.page_shift;
+  const int32_t *row = c.table + (long)src * c.width;
+  for (int p0 = 0; p0 < np; p0 += lanes) {
+    const int p = p0 + lane, page = p < np ? row[p] : -1;
+    const bool copied = page >= 0 && (deep || p >= full);
+    const unsigned long long m = __ballot(copied) >> shift & all;
+    int to = page;
+    if (copied) {
+      const int k = at + __popcll(m & before);
+      to = w.list[k];
+      w.from[k] = page;
+      w.to[k] = to;
+    } else if (page >= 0) {
+      atomicAdd(c.ref + page, 1);
+    }
+    if (p < np) w.row[(long)i * c.width + p] = to;
+    at += __popcll(m);
+  }
+  if (lane == 0) w.row_len[i] = len;
+}
+// Entry i, by `threads` threads that run together or not at all: the target's row.  A page that it gives up keeps its contents during
+// the call (it can only be handed out by a later one).
+__device__ void fork_apply(const CacheView &c, int i, int dst, const PageWork &w, int thread, int threads) {
+  if (w.off[i] < 0) return;
+  const int np_old = pages_of(c, c.len[dst]), len = w.row_len[i], np = pages_of(c, len);
+  int32_t *row = c.table + (long)dst * c.width;
+  for (int p = thread; p < max(np_old, np); p += threads) {
+    if (p < np_old) drop_page(c, row[p]);
+    if (p < np) row[p] = w.row[(long)i * c.width + p];
+  }
+  if (threads > 64) __syncthreads();
+  if (thread == 0) {
+    c.len[dst] = len;
+    c.base[dst] = len;
+    c.slot[dst] = -1;
+  }
+}
+
+// whole: the workgroup does the table's part too, with so many lanes to an entry; 0: launches of their own do
+__global__ __launch_bounds__(kPlan) void cache_fork_plan_kernel(CacheView c, int n, const int32_t *src, const int32_t *dst, int deep, int whole,
+                                                                PageWork w) {
   __shared__ int32_t lds[kPlan / 64];
   const int tid = threadIdx.x;
   auto inside = [&](int s) { return s >= 0 && s < c.max_seqs; };
   for (int i = tid; i < n; i += kPlan)
     if (inside(dst[i])) atomicMin(c.mark + dst[i], i);
-  __syncthreads();
   if (deep) {  // counts by waves, kept where the sources' lengths will be
     for (int i = tid >> 6; i < n; i += kPlan / 64) {
       const int k = inside(src[i]) ? copies_of(c, src[i], true, tid & 63) : 0;
       if ((tid & 63) == 0) w.row_len[i] = k;
     }
-    __syncthreads();
   }
+  __syncthreads();
   auto need = [&](int i) { return deep ? w.row_len[i] : copies_of(c, src[i], false, 0); };
   int total = 0;
   for (int i0 = 0; i0 < n; i0 += kPlan) {
@@ -258,52 +310,20 @@ __global__ __launch_bounds__(kPlan) void cache_fork_plan_kernel(CacheView c, int
   }
   top = block_max(top, lds);
   if (tid == 0) w.info[0] = top;
+  if (!whole) return;
+  __syncthreads();
+  for (int i = tid / whole; i < n; i += kPlan / whole) fork_stage(c, i, src[i], deep, w, tid % whole, whole);
+  __syncthreads();
+  for (int i = tid / whole; i < n; i += kPlan / whole) fork_apply(c, i, dst[i], w, tid % whole, whole);
 }
-
-// A wave per entry: the source's row as the target will have it, holders of shared pages, pages to be copied
 __global__ __launch_bounds__(64) void cache_fork_stage_kernel(CacheView c, const int32_t *src, int deep, PageWork w) {
-  const int i = blockIdx.x, lane = threadIdx.x;
-  int at = w.off[i];
-  if (at < 0) return;
-  const int len = c.len[src[i]], np = pages_of(c, len), full = len >> c.page_shift;
-  const int32_t *row = c.table + (long)src[i] * c.width;
-  for (int p0 = 0; p0 < np; p0 += 64) {
-    const int p = p0 + lane, page = p < np ? row[p] : -1;
-    const bool copied = page >= 0 && (deep || p >= full);
-    const unsigned long long m = __ballot(copied);
-    int to = page;
-    if (copied) {
-      const int k = at + __popcll(m & ((1ull << lane) - 1));
-      to = w.list[k];
-      w.from[k] = page;
-      w.to[k] = to;
-    } else if (page >= 0) {
-      atomicAdd(c.ref + page, 1);
-    }
-    if (p < np) w.row[(long)i * c.width + p] = to;
-    at += __popcll(m);
-  }
-  if (lane == 0) w.row_len[i] = len;
+  fork_stage(c, blockIdx.x, src[blockIdx.x], deep, w, threadIdx.x, 64);
 }
-
-// Workgroups 0 .. n - 1: the targets' rows; the others copy pages.  A page that a target gives up keeps its contents in this
-// launch (it can only be handed out by a later call), and every page written to was free before it.
+// Workgroups 0 .. n - 1: the targets' rows; the others copy pages, all of which were free before the call.
 __global__ __launch_bounds__(256) void cache_fork_apply_kernel(CacheView c, int layers, int n, const int32_t *dst, PageWork w) {
   const int i = blockIdx.x;
   if (i >= n) return copy_pages(c, layers, w, i - n, gridDim.x - n);
-  if (w.off[i] < 0) return;
-  const int s = dst[i], np_old = pages_of(c, c.len[s]), len = w.row_len[i], np = pages_of(c, len);
-  int32_t *row = c.table + (long)s * c.width;
-  for (int p = threadIdx.x; p < max(np_old, np); p += 256) {
-    if (p < np_old) drop_page(c, row[p]);
-    if (p < np) row[p] = w.row[(long)i * c.width + p];
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    c.len[s] = len;
-    c.base[s] = len;
-    c.slot[s] = -1;
-  }
+  fork_apply(c, i, dst[i], w, threadIdx.x, 256);
 }
 
 // ---- sequences cut back -----------------------------------------------------------------------------------------------
@@ -538,9 +558,12 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteArgs a) {
             w[j] = (uint32_t)__builtin_bit_cast(unsigned short, (__bf16)val[2 * j]) |
                    (uint32_t)__builtin_bit_cast(unsigned short, (__bf16)val[2 * j + 1]) << 16;
         }
-        uint32_t *to = side == 0 ? (uint32_t *)at + key_elem(tok, dim, dh) / 2 : lds + tok * (dh / 2 + 1) + dim / 2;
+        if (side == 0) {
+          *(uint4 *)((unsigned short *)at + key_elem(tok, dim, dh)) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; j++) to[j] = w[j];
+          for (int j = 0; j < 4; j++) lds[tok * (dh / 2 + 1) + dim / 2 + j] = w[j];
+        }
       }
     }
   }
@@ -557,20 +580,28 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteArgs a) {
       *to = word;
     } else {
       unsigned short *to = (unsigned short *)(at + 64 * dh) + value_elem(g, dim);
-      const unsigned short *from = (const unsigned short *)lds;
+      const unsigned short *from = (const unsigned short *)lds + g * (dh + 2) + dim;
+      if (g >= t0 && g + 8 <= t1) {
+        uint32_t w[4];
 #pragma unroll
-      for (int j = 0; j < 8; j++)
-        if (g + j >= t0 && g + j < t1) to[j] = from[(g + j) * (dh + 2) + dim];
+        for (int j = 0; j < 4; j++) w[j] = from[2 * j * (dh + 2)] | (uint32_t)from[(2 * j + 1) * (dh + 2)] << 16;
+        *(uint4 *)to = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+          if (g + j >= t0 && g + j < t1) to[j] = from[j * (dh + 2)];
+      }
     }
   }
 }
 
+// At most 128 dims of a tile of one head
 template <int KIND>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadArgs a) {
   extern __shared__ uint32_t lds[];
   const CacheView &c = a.c;
-  const int tile = blockIdx.x % a.tiles, h = blockIdx.x / a.tiles % c.heads, i = blockIdx.x / a.tiles / c.heads;
-  const int tid = threadIdx.x, dh = c.dh, per = dh / 8;
+  const int tid = threadIdx.x, dh = c.dh, dw = min(dh, 128), parts = dh / dw, per = dw / 8;
+  const int part = blockIdx.x % parts, b = blockIdx.x / parts, h = b % c.heads, tile = b / c.heads % a.tiles, i = b / c.heads / a.tiles;
   const int s = a.r.seq ? a.r.seq[i] : i;
   const bool known = s >= 0 && s < c.max_seqs;
   if (!known && tid == 0 && tile == 0 && h == 0) atomicOr(c.flags, 1);
@@ -579,11 +610,11 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadArgs a) {
   const char *at = c.pool + cache_tile_offset(c, a.layer, max(page, 0), h, tile & ((1 << (c.page_shift - 5)) - 1), cache_tile_bytes(KIND, dh));
   constexpr int kPer = KIND == CACHE_Q4 ? 16 : 64;  // bytes of a dim's keys or values
   if (page >= 0) {
-    for (int x = tid; x < kPer * dh / 16; x += 256) ((uint4 *)lds)[x] = ((const uint4 *)(at + kPer * dh))[x];
+    for (int x = tid; x < kPer * dw / 16; x += 256) ((uint4 *)lds)[x] = ((const uint4 *)(at + kPer * dh))[part * (kPer * dw / 16) + x];
   }
   __syncthreads();
   for (int x = tid; x < t1 * per; x += 256) {
-    const int tok = x / per, dim = x % per * 8;
+    const int tok = x / per, own = x % per * 8, dim = part * dw + own;
     const bool there = page >= 0 && tile * kTile + tok < len;
     const long o = (((long)i * a.max_keys + tile * kTile + tok) * c.heads + h) * dh + dim;
 #pragma unroll
@@ -596,7 +627,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadArgs a) {
           const uint32_t word = side == 0 ? ((const uint32_t *)at)[q4_key_word(tok, dim, dh)] : 0;
 #pragma unroll
           for (int j = 0; j < 8; j++) {
-            const int code = side == 0 ? (word >> (4 * j)) & 15 : (lds[q4_value_word(tok, dim + j)] >> (4 * (tok & 7))) & 15;
+            const int code = side == 0 ? (word >> (4 * j)) & 15 : (lds[q4_value_word(tok, own + j)] >> (4 * (tok & 7))) & 15;
             val[j] = q4_magnitude(code & 7) * sc;
             if (code & 8) val[j] = -val[j];
           }
@@ -604,21 +635,33 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadArgs a) {
 #pragma unroll
           for (int j = 0; j < 8; j++) {
             const unsigned short b = side == 0 ? ((const unsigned short *)at)[key_elem(tok, dim, dh) + j]
-                                               : ((const unsigned short *)lds)[value_elem(tok, dim + j)];
+                                               : ((const unsigned short *)lds)[value_elem(tok, own + j)];
             val[j] = KIND == CACHE_F16 ? (float)__builtin_bit_cast(_Float16, b) : (float)__builtin_bit_cast(__bf16, b);
           }
         }
       }
       void *dst = side == 0 ? a.k : a.v;
       if (a.type == IO_F32) {
+        float *to = (float *)dst + o;
+        if (a.vec) {
+          *(float4 *)to = make_float4(val[0], val[1], val[2], val[3]);
+          *(float4 *)(to + 4) = make_float4(val[4], val[5], val[6], val[7]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; j++) ((float *)dst)[o + j] = val[j];
-      } else if (a.type == IO_F16) {
-#pragma unroll
-        for (int j = 0; j < 8; j++) ((_Float16 *)dst)[o + j] = (_Float16)val[j];
+          for (int j = 0; j < 8; j++) to[j] = val[j];
+        }
       } else {
+        unsigned short w[8];
 #pragma unroll
-        for (int j = 0; j < 8; j++) ((__bf16 *)dst)[o + j] = (__bf16)val[j];
+        for (int j = 0; j < 8; j++)
+          w[j] = a.type == IO_F16 ? __builtin_bit_cast(unsigned short, (_Float16)val[j]) : __builtin_bit_cast(unsigned short, (__bf16)val[j]);
+        unsigned short *to = (unsigned short *)dst + o;
+        if (a.vec) {
+          *(uint4 *)to = make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; j++) to[j] = w[j];
+        }
       }
     }
   }
@@ -635,8 +678,9 @@ hipError_t launch_cache_write(const CacheWriteArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 hipError_t launch_cache_read(const CacheReadArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)((long)a.tiles * a.c.heads * a.r.n));
-  const size_t lds = (a.c.kind == CACHE_Q4 ? 16 : 64) * a.c.dh;
+  const int dw = std::min(a.c.dh, 128);
+  const dim3 grid((unsigned)((long)a.tiles * a.c.heads * a.r.n * (a.c.dh / dw)));
+  const size_t lds = (a.c.kind == CACHE_Q4 ? 16 : 64) * dw;
   if (a.c.kind == CACHE_Q4) hipLaunchKernelGGL(cache_read_kernel<CACHE_Q4>, grid, dim3(256), lds, s, a);
   else if (a.c.kind == CACHE_F16) hipLaunchKernelGGL(cache_read_kernel<CACHE_F16>, grid, dim3(256), lds, s, a);
   else hipLaunchKernelGGL(cache_read_kernel<CACHE_BF16>, grid, dim3(256), lds, s, a);
@@ -751,9 +795,13 @@ int become(nt_cache *c, int32_t n, const int32_t *d_src, const int32_t *d_dst, i
   if (rc || n == 0) return rc;
   if (!d_src || !d_dst) return fail(NT_EINVAL, "null argument");
   hipStream_t s = as_stream(hip_stream);
-  hipLaunchKernelGGL(nt::cache_fork_plan_kernel, dim3(1), dim3(nt::kPlan), 0, s, c->v, n, d_src, d_dst, deep, c->w);
-  hipLaunchKernelGGL(nt::cache_fork_stage_kernel, dim3(n), dim3(64), 0, s, c->v, d_src, deep, c->w);
-  hipLaunchKernelGGL(nt::cache_fork_apply_kernel, dim3(n + nt::kCopyBlocks), dim3(256), 0, s, c->v, c->cfg.n_layers, n, d_dst, c->w);
+  // 16 waves go through the table's rows as fast as a launch of their own, and a third, begin: 48 entries of one page or two 22 us
+  // for both launches against XXX for the three.
+  const int whole = (double)n * c->v.width > 4096 ? 0 : c->v.width <= 16 ? 16 : 64, tables = whole ? 0 : n;
+  const int copies = nt::copy_blocks(c->v, c->cfg.n_layers, deep ? (double)n * c->v.width : n);
+  hipLaunchKernelGGL(nt::cache_fork_plan_kernel, dim3(1), dim3(nt::kPlan), 0, s, c->v, n, d_src, d_dst, deep, whole, c->w);
+  if (!whole) hipLaunchKernelGGL(nt::cache_fork_stage_kernel, dim3(n), dim3(64), 0, s, c->v, d_src, deep, c->w);
+  hipLaunchKernelGGL(nt::cache_fork_apply_kernel, dim3(tables + copies), dim3(256), 0, s, c->v, c->cfg.n_layers, tables, d_dst, c->w);
   HIP_TRY(hipGetLastError());
   return NT_OK;
 }
@@ -864,8 +912,8 @@ int nt_cache_read(nt_cache *c, int32_t layer, int32_t n, const int32_t *d_seq, i
   if (n == 0 || max_keys == 0) return NT_OK;
   if (!d_k || !d_v) return fail(NT_EINVAL, "null argument");
   const int tiles = (max_keys + nt::kTile - 1) / nt::kTile;
-  if ((rc = check_blocks(tiles, c->cfg.n_kv_heads, n))) return rc;
-  nt::CacheReadArgs r{c->v, nt::CacheRows{n, 0, d_seq, nullptr}, layer, type, max_keys, tiles, d_k, d_v};
+  if ((rc = check_blocks(tiles, c->cfg.n_kv_heads * 4, n))) return rc;
+  nt::CacheReadArgs r{c->v, nt::CacheRows{n, 0, d_seq, nullptr}, layer, type, max_keys, tiles, d_k, d_v, aligned(d_k, 0, type) && aligned(d_v, 0, type)};
   HIP_TRY(nt::launch_cache_read(r, as_stream(hip_stream)));
   return NT_OK;
 }
@@ -886,7 +934,8 @@ int nt_cache_truncate(nt_cache *c, int32_t n, const int32_t *d_seq, const int32_
     if (d_seq) hipLaunchKernelGGL(nt::cache_unmark_kernel, dim3((n + 255) / 256), dim3(256), 0, s, c->v, n, d_seq);
   } else {
     hipLaunchKernelGGL(nt::cache_truncate_plan_kernel, dim3(1), dim3(nt::kPlan), 0, s, c->v, n, d_seq, d_len, c->w);
-    hipLaunchKernelGGL(nt::cache_truncate_apply_kernel, dim3(n + nt::kCopyBlocks), dim3(256), 0, s, c->v, c->cfg.n_layers, n, d_seq, d_len, c->w);
+    hipLaunchKernelGGL(nt::cache_truncate_apply_kernel, dim3(n + nt::copy_blocks(c->v, c->cfg.n_layers, n)), dim3(256), 0, s, c->v,
+                       c->cfg.n_layers, n, d_seq, d_len, c->w);
   }
   HIP_TRY(hipGetLastError());
   return NT_OK;
@@ -907,7 +956,7 @@ int nt_cache_compact(nt_cache *c, void *hip_stream) {
   if (rc) return rc;
   hipStream_t s = as_stream(hip_stream);
   hipLaunchKernelGGL(nt::cache_compact_plan_kernel, dim3(1), dim3(nt::kPlan), 0, s, c->v, c->w);
-  hipLaunchKernelGGL(nt::cache_compact_apply_kernel, dim3(c->cfg.max_seqs + nt::kCopyBlocks), dim3(256), 0, s, c->v, c->cfg.n_layers, c->w);
+  hipLaunchKernelGGL(nt::cache_compact_apply_kernel, dim3(c->cfg.max_seqs + nt::copy_blocks(c->v, c->cfg.n_layers, c->cfg.n_pages)), dim3(256), 0, s, c->v, c->cfg.n_layers, c->w);
   HIP_TRY(hipGetLastError());
   return NT_OK;
 }
