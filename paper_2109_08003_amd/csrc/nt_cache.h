@@ -81,17 +81,18 @@ struct CacheAttnArgs {
   int32_t vec, vec_out;  // query rows, output rows are 16-byte aligned
   float *part;           // [share][row][dh], behind them {maximum, sum} [share][row]
   long part_floats;
-  // set by the launchers: tiles of query rows of a sequence, workgroups that share their keys, tiles of keys that each has at
-  // least, rows of a share
-  int32_t row_tiles, splits, least, part_rows;
+  // set by the launchers: tiles of query rows of a sequence and their rows, workgroups that share their keys, tiles of keys that
+  // each has at least, rows that a share leaves room for
+  int32_t row_tiles, tile_rows, splits, least, part_rows;
   float2 *part_sums;
 };
 constexpr int kMaxSplits = 64;  // shares of one row's keys: a lane each in the join
-constexpr long kPartFloats = 8l << 20;  // what the shares of a call leave for the join, at most: 16,000 of 4 rows of 128
+constexpr long kPartFloats = 16l << 20;  // what the shares of a call leave for the join, at most: 512 of 192 rows of 128, 32,000 of four
 // Queries in tiles of 8 (rows: token, then head of the group), each split over the keys, of which a row sees about `tiles` tiles.
 hipError_t launch_cache_token(CacheAttnArgs a, long tiles, hipStream_t s);
-// Tiles of 128 to 256 query rows, unsplit.
-hipError_t launch_cache_prompt(const CacheAttnArgs &a, hipStream_t s);
+// Tiles of 128 or 192 query rows, likewise
+hipError_t launch_cache_prompt(CacheAttnArgs a, long tiles, hipStream_t s);
+hipError_t launch_cache_join(const CacheAttnArgs &a, hipStream_t s);  // what the shares of either have left
 
 #ifdef __HIPCC__
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));

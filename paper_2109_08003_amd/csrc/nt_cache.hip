@@ -761,8 +761,9 @@ size_t lay_out(nt_cache *c, char *base) {
   v.ref = ints(g.n_pages); v.used = (uint32_t *)ints((g.n_pages + 31) / 32); v.flags = ints(2);
   c->w.off = ints(g.max_seqs); c->w.list = ints(g.n_pages); c->w.from = ints(g.n_pages); c->w.to = ints(g.n_pages);
   c->w.info = ints(2); c->w.row_len = ints(g.max_seqs); c->w.row = ints((size_t)g.max_seqs * v.width);
-  // for the most shares that single tokens of all sequences can have
-  c->part_floats = (long)std::min<double>(nt::kPartFloats, (double)g.max_seqs * g.n_q_heads * nt::kMaxSplits * (g.d_head + 2)) & ~3l;
+  // for the most shares that single tokens of all sequences can have; more, for shares of prompts, where the pool is larger
+  const double tokens = (double)g.max_seqs * g.n_q_heads * nt::kMaxSplits * (g.d_head + 2);
+  c->part_floats = (long)std::min<double>(nt::kPartFloats, std::max(tokens, (double)v.layer_bytes * g.n_layers / 4)) & ~3l;
   c->part = (float *)take((size_t)c->part_floats * 4);
   return off;
 }
@@ -996,7 +997,11 @@ hipError_t nt::cache_end(nt_cache *c, int n, const int32_t *seq, hipStream_t s) 
 hipError_t nt::cache_write(nt_cache *c, int layer, const CacheRows &r, const void *k, const void *v, long ld, int type, hipStream_t s) {
   return launch_cache_write(CacheWriteArgs{c->v, r, layer, type, write_tiles(r.max_new), k, v, ld, aligned(k, ld, type) && aligned(v, ld, type)}, s);
 }
-// Attention by the kernel that fits
+// Attention by the kernel that fits.  The one for few rows reads the keys and values once for every eight rows, the one for many once
+// for 128 or 192 but computes as many: 8 sequences of 16,000 tokens, 32 / 8 heads of 128, with 8 / 16 / 32 / 64 rows to a key/value
+// head 117 / 166 / 283 / 519 us and 138 / 135 / 135 / 149; in 4 bits, where a tile is a quarter of the bytes, 51 / 88 / 146 / 268 and
+// 137 / 139 / 140 / 151; 64 of 200 tokens, one head of 512, 2 / 4 / 8 / 16 rows 17 / 21 / 30 / 40 and 27 / 27 / 27 / 29.
+constexpr int kFewRows = 8, kFewRowsQ4 = 16;
 hipError_t nt::cache_attend(nt_cache *c, const nt_attend_args &a, int out_type, long lo_offset, hipStream_t s) {
   const nt_cache_config &g = c->cfg;
   CacheAttnArgs k{};
@@ -1009,8 +1014,9 @@ hipError_t nt::cache_attend(nt_cache *c, const nt_attend_args &a, int out_type, 
   k.q = a.q; k.out = a.out; k.ld_q = a.ld_q; k.ld_out = a.ld_out; k.lo_offset = lo_offset;
   k.scale = a.scale; k.window = a.window; k.sinks = a.sinks; k.vec = aligned(a.q, a.ld_q, a.type); k.vec_out = aligned(a.out, a.ld_out, a.type);
   k.part = c->part; k.part_floats = c->part_floats;
-  if ((long)a.max_new * k.group > 64) return launch_cache_prompt(k, s);
   long keys = a.max_keys > 0 ? std::min(a.max_keys, g.max_len) : g.max_len;
   if (a.window > 0) keys = std::min<long>(keys, (long)a.window + a.sinks + a.max_new + 2 * kTile);
-  return launch_cache_token(k, (keys + kTile - 1) / kTile, s);
+  const long tiles = (keys + kTile - 1) / kTile;
+  const bool many = a.max_new > 1 && (long)a.max_new * k.group > (g.kind == NT_CACHE_Q4 ? kFewRowsQ4 : kFewRows);
+  return many ? launch_cache_prompt(k, tiles, s) : launch_cache_token(k, tiles, s);
 }

@@ -19,39 +19,6 @@ constexpr int kRows = 8, kWaves = 4, kFill = 1024;
 // wave would leave one wave to a SIMD.  Their parts of the scores are added through the LDS.
 constexpr int parts_of(int dh) { return dh > 128 ? dh / 128 : 1; }
 
-// What a workgroup has to do: the rows of sequence i in row tile rt, the tiles of keys that one of them sees (those of the sinks, then
-// those of the window), and how they are shared out.
-struct Share {
-  int s, len, m, R;                        // sequence, its length, new tokens, query rows
-  long row0;
-  int first, p_min, p_max, low;            // positions: of the first new token, of the rows; first key of the earliest window
-  int sink_tiles, window_tile, tiles, per, shares;
-  bool known;
-  __device__ __forceinline__ Share(const CacheAttnArgs &a, int i, int rt) {
-    s = a.r.seq ? a.r.seq[i] : i;
-    row0 = a.r.first ? a.r.first[i] : i;
-    m = a.r.first ? a.r.first[i + 1] - (int)row0 : 1;
-    known = s >= 0 && s < a.c.max_seqs;
-    len = known ? a.c.len[s] : 0;
-    R = min(m, a.r.max_new) * a.group;
-    first = len - m;
-    p_min = first + rt * kRows / a.group;
-    p_max = first + min(rt * kRows + kRows - 1, R - 1) / a.group;
-    low = a.window > 0 ? max(p_min - a.window + 1, 0) : 0;
-    sink_tiles = (min(a.sinks, low) + kTile - 1) / kTile;
-    window_tile = max(low / kTile, sink_tiles);
-    tiles = p_max < 0 ? 0 : sink_tiles + max(p_max / kTile + 1 - window_tile, 0);
-    per = max((tiles + a.splits - 1) / a.splits, a.least);
-    shares = max((tiles + per - 1) / per, 1);
-  }
-};
-
-// x / l, zero where no key was seen
-__device__ __forceinline__ void store_row(const CacheAttnArgs &a, const Share &w, int h, int row, int d, int dh, float x, float l) {
-  if (row < w.R)
-    io_store(a.out, a.out_type, (w.row0 + row / a.group) * a.ld_out + (long)(h * a.group + row % a.group) * dh + d, a.lo_offset, l == 0.f ? 0.f : x / l);
-}
-
 // ONE: every sequence has one new token, so the rows of a workgroup see the same keys
 template <int KIND, int DH, bool ONE>
 __global__ __launch_bounds__(256, (ONE ? 2 : 1)) void cache_token_kernel(CacheAttnArgs a) {
@@ -68,7 +35,7 @@ __global__ __launch_bounds__(256, (ONE ? 2 : 1)) void cache_token_kernel(CacheAt
   const int part = wave % PARTS, mine = wave / PARTS;  // of a tile's dims, of the tiles in work
   const int split = blockIdx.x % a.splits, group = blockIdx.x / a.splits, h = group % c.heads, rt = group / c.heads % a.row_tiles,
             i = group / c.heads / a.row_tiles;
-  const Share w(a, i, rt);
+  const Share w(a, i, rt, kRows);
   const int G = a.group;
   if ((!w.known || w.m < 0 || w.m > a.r.max_new || w.m > w.len) && split == 0 && h == 0 && rt == 0 && tid == 0) atomicOr(c.flags, 1);
   if (rt * kRows >= w.R || split >= w.shares) return;
@@ -259,17 +226,17 @@ __global__ __launch_bounds__(256, (ONE ? 2 : 1)) void cache_token_kernel(CacheAt
   }
 }
 
-// Joins the shares of a row: a workgroup per tile of rows
+// Joins the shares of eight rows of a tile
 template <int DH>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
   __shared__ float lds_f[kRows][kMaxSplits], lds_l[kRows];
-  const int tid = threadIdx.x, lane = tid & 63, group = blockIdx.x;
-  const int h = group % a.c.heads, rt = group / a.c.heads % a.row_tiles, i = group / a.c.heads / a.row_tiles;
-  const Share w(a, i, rt);
-  if (rt * kRows >= w.R || w.shares == 1) return;
-  const long at = (long)group * a.splits * a.part_rows;
+  const int tid = threadIdx.x, lane = tid & 63, chunks = (a.tile_rows + kRows - 1) / kRows, group = blockIdx.x / chunks;
+  const int h = group % a.c.heads, rt = group / a.c.heads % a.row_tiles, i = group / a.c.heads / a.row_tiles, r0 = blockIdx.x % chunks * kRows;
+  const Share w(a, i, rt, a.tile_rows);
+  const int first = rt * a.tile_rows + r0, rows = min(min(w.R - first, kRows), a.tile_rows - r0);
+  if (rows <= 0 || w.shares == 1) return;
+  const long at = (long)group * a.splits * a.part_rows + r0;
   static_assert(kMaxSplits == 64, "a share per lane");
-  const int rows = min(w.R - rt * kRows, kRows);
   for (int r = tid >> 6; r < rows; r += 4) {  // weights of the shares
     const float2 ml = lane < w.shares ? a.part_sums[at + lane * a.part_rows + r] : make_float2(kLowest, 0.f);
     const float mx = wave_max(ml.x), f = __builtin_amdgcn_exp2f(ml.x - mx), l = wave_sum(f * ml.y);
@@ -284,7 +251,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
 #pragma unroll 8
     for (int k = 0; k < w.shares; k++) y += lds_f[r][k] * from[(long)k * a.part_rows * DH / 4];
 #pragma unroll
-    for (int k = 0; k < 4; k++) store_row(a, w, h, rt * kRows + r, d + k, DH, y[k], lds_l[r]);
+    for (int k = 0; k < 4; k++) store_row(a, w, h, first + r, d + k, DH, y[k], lds_l[r]);
   }
 }
 
@@ -295,6 +262,7 @@ hipError_t launch(CacheAttnArgs a, long tiles, hipStream_t s) {
   // two shares and 218 with 15; 256 in 4 bits 391 with one and 291 with 7.  Turns 2 / 4 / 8 / 16: 225 / 220 / 218 / 221, 304 / 300 / 291 / 283.
   constexpr int kTurns = 8;
   const long groups = (long)a.c.heads * a.row_tiles * a.r.n, at_once = kWaves / parts_of(DH);
+  a.tile_rows = kRows;
   a.part_rows = (int)std::min<long>(kRows, (long)a.r.max_new * a.group);
   const long slots = a.part_floats / (a.part_rows * (DH + 2)), turns = (tiles + at_once - 1) / at_once;
   const long few = std::min(kFill / groups, turns), many = std::min(slots / groups, turns / kTurns);
@@ -304,8 +272,8 @@ hipError_t launch(CacheAttnArgs a, long tiles, hipStream_t s) {
   const dim3 grid((unsigned)(groups * a.splits)), block(256);
   if (a.r.max_new == 1) hipLaunchKernelGGL((cache_token_kernel<KIND, DH, true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((cache_token_kernel<KIND, DH, false>), grid, block, 0, s, a);
-  if (a.splits > 1) hipLaunchKernelGGL(cache_join_kernel<DH>, dim3((unsigned)groups), block, 0, s, a);
-  return hipGetLastError();
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || a.splits == 1 ? e : launch_cache_join(a, s);
 }
 
 template <int KIND>
@@ -320,6 +288,16 @@ hipError_t launch_width(const CacheAttnArgs &a, long tiles, hipStream_t s) {
 
 }  // namespace
 
+hipError_t launch_cache_join(const CacheAttnArgs &a, hipStream_t s) {
+  const dim3 grid((unsigned)((long)a.r.n * a.c.heads * a.row_tiles * ((a.tile_rows + kRows - 1) / kRows))), block(256);
+  switch (a.c.dh) {
+    case 64: hipLaunchKernelGGL(cache_join_kernel<64>, grid, block, 0, s, a); break;
+    case 128: hipLaunchKernelGGL(cache_join_kernel<128>, grid, block, 0, s, a); break;
+    case 256: hipLaunchKernelGGL(cache_join_kernel<256>, grid, block, 0, s, a); break;
+    default: hipLaunchKernelGGL(cache_join_kernel<512>, grid, block, 0, s, a);
+  }
+  return hipGetLastError();
+}
 hipError_t launch_cache_token(CacheAttnArgs a, long tiles, hipStream_t s) {
   a.row_tiles = (int)(((long)a.r.max_new * a.group + kRows - 1) / kRows);
   if (a.c.kind == CACHE_Q4) return launch_width<CACHE_Q4>(a, tiles, s);

@@ -10,6 +10,39 @@ namespace nt {
 constexpr float kSlack = 8.f;
 constexpr float kLowest = -1e38f;  // maximum of no score; less than any that is a number
 
+// What a workgroup has to do: the rows of sequence i in row tile rt of `rows` rows, the tiles of keys that one of them sees (those of the sinks, then
+// those of the window), and how they are shared out.
+struct Share {
+  int s, len, m, R;                        // sequence, its length, new tokens, query rows
+  long row0;
+  int first, p_min, p_max, low;            // positions: of the first new token, of the rows; first key of the earliest window
+  int sink_tiles, window_tile, tiles, per, shares;
+  bool known;
+  __device__ __forceinline__ Share(const CacheAttnArgs &a, int i, int rt, int rows) {
+    s = a.r.seq ? a.r.seq[i] : i;
+    row0 = a.r.first ? a.r.first[i] : i;
+    m = a.r.first ? a.r.first[i + 1] - (int)row0 : 1;
+    known = s >= 0 && s < a.c.max_seqs;
+    len = known ? a.c.len[s] : 0;
+    R = min(m, a.r.max_new) * a.group;
+    first = len - m;
+    p_min = first + rt * rows / a.group;
+    p_max = first + min(rt * rows + rows - 1, R - 1) / a.group;
+    low = a.window > 0 ? max(p_min - a.window + 1, 0) : 0;
+    sink_tiles = (min(a.sinks, low) + kTile - 1) / kTile;
+    window_tile = max(low / kTile, sink_tiles);
+    tiles = p_max < 0 ? 0 : sink_tiles + max(p_max / kTile + 1 - window_tile, 0);
+    per = max((tiles + a.splits - 1) / a.splits, a.least);
+    shares = max((tiles + per - 1) / per, 1);
+  }
+};
+
+// x / l, zero where no key was seen
+__device__ __forceinline__ void store_row(const CacheAttnArgs &a, const Share &w, int h, int row, int d, int dh, float x, float l) {
+  if (row < w.R)
+    io_store(a.out, a.out_type, (w.row0 + row / a.group) * a.ld_out + (long)(h * a.group + row % a.group) * dh + d, a.lo_offset, l == 0.f ? 0.f : x / l);
+}
+
 template <int KIND> struct FragType { typedef f16x8 type; typedef _Float16 elem; };
 template <> struct FragType<CACHE_BF16> { typedef bf16x8 type; typedef __bf16 elem; };
 

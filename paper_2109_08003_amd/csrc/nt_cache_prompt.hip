@@ -5,6 +5,7 @@
 // that go there directly; 4-bit ones rounded back to fp16 once for all waves) while each computes on the present one for its own
 // NQ x 16 rows, with the running maximum and sum of the softmax in registers.  As in the kernel for few rows, scores are S^T = K Q^T
 // and weights enter O^T = V^T P^T from the registers they are made in.
+#include <algorithm>
 #include <climits>
 
 #include "nt_cache_frag.h"
@@ -12,7 +13,7 @@
 namespace nt {
 namespace {
 
-typedef __attribute__((address_space(3))) char lds_char;
+constexpr long kFill = 512;  // workgroups that the chip holds at once
 
 // Rows of a wave in tiles of 16, waves, tiles of keys in a stage.  Accumulators, queries, scores and weights of a wave are
 // NQ (DH / 4 + DH / 8 + 12) registers, 256 for two waves per SIMD; a fragment read from the LDS serves NQ products of 16 clocks,
@@ -39,24 +40,19 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
   extern __shared__ __align__(1024) char lds[];  // [2][ST][TB], before that the queries
   const CacheView &c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g4 = lane >> 4, G = a.group;
-  // row tiles of a head's sequence follow one another on one of the eight dies, whose cache they share; long ones first
-  const int b = blockIdx.x, j = spread ? b / 8 : b;
-  const int unit = spread ? j / a.row_tiles * 8 + b % 8 : j / a.row_tiles, rt = a.row_tiles - 1 - j % a.row_tiles;
+  // row tiles of a head's sequence, and their shares, follow one another on one of the eight dies, whose cache they share; long ones
+  // first
+  const int b = blockIdx.x, j = spread ? b / 8 : b, split = j % a.splits, jt = j / a.splits;
+  const int unit = spread ? jt / a.row_tiles * 8 + b % 8 : jt / a.row_tiles, rt = a.row_tiles - 1 - jt % a.row_tiles;
   const int h = unit % c.heads, i = unit / c.heads;
   if (i >= a.r.n) return;
-  const int s = a.r.seq ? a.r.seq[i] : i;
-  const long row0 = a.r.first ? a.r.first[i] : i;
-  const int m = a.r.first ? a.r.first[i + 1] - (int)row0 : 1;
-  const bool known = s >= 0 && s < c.max_seqs;
-  const int len = known ? c.len[s] : 0, R = min(m, a.r.max_new) * G;
-  if ((!known || m < 0 || m > a.r.max_new || m > len) && h == 0 && rt == 0 && tid == 0) atomicOr(c.flags, 1);
-  if (rt * ROWS >= R) return;
-  // as Share in the kernel for few rows
-  const int first = len - m, p_min = first + rt * ROWS / G, p_max = first + min(rt * ROWS + ROWS - 1, R - 1) / G;
-  const int low = a.window > 0 ? max(p_min - a.window + 1, 0) : 0;
-  const int sink_tiles = (min(a.sinks, low) + kTile - 1) / kTile, window_tile = max(low / kTile, sink_tiles);
-  const int tiles = p_max < 0 ? 0 : sink_tiles + max(p_max / kTile + 1 - window_tile, 0), stages = (tiles + ST - 1) / ST;
-  auto tile_of = [&](int t) { return t < sink_tiles ? t : window_tile + t - sink_tiles; };
+  const Share w(a, i, rt, ROWS);
+  const int s = w.s, R = w.R, first = w.first, p_min = w.p_min, p_max = w.p_max, low = w.low;
+  const long row0 = w.row0;
+  if ((!w.known || w.m < 0 || w.m > a.r.max_new || w.m > w.len) && h == 0 && rt == 0 && split == 0 && tid == 0) atomicOr(c.flags, 1);
+  if (rt * ROWS >= R || split >= w.shares) return;
+  const int t0 = split * w.per, tiles = min(t0 + w.per, w.tiles), stages = (max(tiles - t0, 0) + ST - 1) / ST;
+  auto tile_of = [&](int t) { return t < w.sink_tiles ? t : w.window_tile + t - w.sink_tiles; };
 
   // queries: rounded to the cache's type in the LDS, in the order in which the waves read them back.  A power of two brings the
   // largest of each to 1 .. 2: no overflow in fp16.
@@ -115,7 +111,7 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
 #pragma unroll
     for (int x = 0; x < ST; x++) {
       if (page[x] < 0) continue;
-      const char *at = address(stage * ST + x, page[x]);
+      const char *at = address(t0 + stage * ST + x, page[x]);
       if constexpr (KIND != CACHE_Q4) {
         for (int k = wave; k < TB / 1024; k += NW)
           __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(at + k * 1024 + lane * 16),
@@ -131,7 +127,7 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
         for (int z = 0; z < ST; z++)
           if (x == z) pg = page[z];
         if (pg < 0) continue;
-        const char *at = address(stage * ST + x, pg);
+        const char *at = address(t0 + stage * ST + x, pg);
         code[y] = *(const uint4 *)(at + p * 1024 + lane * 16);
         if (p < PIECES / 2) {  // keys: words 4 p .. 4 p + 3
           const int tok = 8 * (col >> 2) + (col & 3);
@@ -192,7 +188,7 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
   uint32_t present = 0, present_next = 0;  // bit x: tile x of the stage has a page
   auto look_up = [&](int stage) {
 #pragma unroll
-    for (int x = 0; x < ST; x++) next[x] = page_of(stage * ST + x);
+    for (int x = 0; x < ST; x++) next[x] = page_of(t0 + stage * ST + x);
   };
   auto mask_of = [&]() {
     uint32_t b = 0;
@@ -232,15 +228,15 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
     look_up(stage + 2);
     bool cleaned = false;
     for (int x = 0; x < ST; x++) {
-      const int j0 = tile_of(stage * ST + x) * kTile;
-      if (!(present >> x & 1) || stage * ST + x >= tiles || seen_by_all(j0)) continue;
+      const int j0 = tile_of(t0 + stage * ST + x) * kTile;
+      if (!(present >> x & 1) || t0 + stage * ST + x >= tiles || seen_by_all(j0)) continue;
       clean(j0, lds + (buf * ST + x) * TB);
       cleaned = true;
     }
     if (cleaned) __syncthreads();
 #pragma unroll 1
     for (int x = 0; x < ST; x++) {
-      const int j0 = tile_of(stage * ST + x) * kTile;
+      const int j0 = tile_of(t0 + stage * ST + x) * kTile;
       // nothing for this wave
       if (!(present >> x & 1) || j0 > w_max || (j0 + kTile <= w_low && j0 >= a.sinks)) continue;
       const bool all_seen = j0 + kTile - 1 <= w_min && (a.window == 0 || j0 >= w_max - a.window + 1 || j0 + kTile <= a.sinks);
@@ -313,12 +309,20 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
     present = present_next;
     __syncthreads();
   }
+  const long part0 = ((long)((i * a.row_tiles + rt) * c.heads + h) * a.splits + split) * a.part_rows;
 #pragma unroll
   for (int k = 0; k < NQ; k++) {
     const int row = wave_row + k * 16 + col;
     float l = wave_pair16(sum[k], sum[k], WaveAdd{});
     l = wave_pair32(l, l, WaveAdd{});
     if (row >= R) continue;
+    if (w.shares > 1) {
+      const long r = part0 + row - rt * ROWS;
+#pragma unroll
+      for (int n = 0; n < NV; n++) *(f32x4 *)(a.part + r * DH + n * 16 + g4 * 4) = o[k][n];
+      if (g4 == 0) a.part_sums[r] = make_float2(top[k], l);
+      continue;
+    }
     const long at = (row0 + row / G) * a.ld_out + (long)(h * G + row % G) * DH + g4 * 4;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     auto rows = [&](auto *out) {
@@ -345,7 +349,7 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
   }
   if (!lds_strange) return;
   // The infinities and NaN that were left out reach the rows that see them: a lane corrects what it has stored.
-  for (int t = 0; t < tiles; t++) {
+  for (int t = t0; t < tiles; t++) {
     const int pg = page_of(t), j0 = tile_of(t) * kTile;
     if (pg < 0 || seen_by_all(j0)) continue;
     const char *at = address(t, pg);
@@ -363,44 +367,56 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
         for (int k = 0; k < NQ; k++) {
           const int row = wave_row + k * 16 + col, p = row < R ? first + row / G : -1;
           if (j0 + key > p || (a.window > 0 && j0 + key < p - a.window + 1 && j0 + key >= a.sinks)) continue;
-          const long o = (row0 + row / G) * a.ld_out + (long)(h * G + row % G) * DH + dim;
-          io_store(a.out, a.out_type, o, 0, io_load(a.out, a.out_type, o) + v);
+          if (w.shares > 1) {
+            a.part[(part0 + row - rt * ROWS) * DH + dim] += v;
+          } else {
+            const long o = (row0 + row / G) * a.ld_out + (long)(h * G + row % G) * DH + dim;
+            io_store(a.out, a.out_type, o, 0, io_load(a.out, a.out_type, o) + v);
+          }
         }
       }
   }
 }
 
 template <int KIND, int DH>
-hipError_t launch(CacheAttnArgs a, hipStream_t s) {
+hipError_t launch(CacheAttnArgs a, long tiles, hipStream_t s) {
   typedef PromptShape<DH> P;
   constexpr int kRows = P::NW * P::NQ * 16, kStages = 2 * P::ST * 128 * DH, kQueries = kRows * DH * 2;
   constexpr int kLds = kStages > kQueries ? kStages : kQueries;  // first the queries, then the stages
   static const hipError_t limit = hipFuncSetAttribute((const void *)cache_prompt_kernel<KIND, DH>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
   if (limit != hipSuccess) return limit;
   a.row_tiles = (int)(((long)a.r.max_new * a.group + kRows - 1) / kRows);
-  const long units = (long)a.r.n * a.c.heads;
+  const long units = (long)a.r.n * a.c.heads, groups = units * a.row_tiles;
+  // Shares of the keys where there are fewer workgroups than the chip holds, two to a CU, of kTurns tiles at least.
+  constexpr int kTurns = 8;
+  a.tile_rows = a.part_rows = kRows;
+  const long slots = a.part_floats / (kRows * (DH + 2));
+  a.splits = (int)std::max<long>(1, std::min({kFill / groups, tiles / kTurns, slots / groups, (long)kMaxSplits}));
+  a.least = kTurns;
+  a.part_sums = (float2 *)(a.part + slots * kRows * DH);
   // spread over the dies by unit where that leaves none idle
   const int spread = units % 8 == 0 || units >= 64;
-  const long blocks = (spread ? (units + 7) / 8 * 8 : units) * a.row_tiles;
+  const long blocks = (spread ? (units + 7) / 8 * 8 : units) * a.row_tiles * a.splits;
   hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH>), dim3((unsigned)blocks), dim3(P::NW * 64), kLds, s, a, spread);
-  return hipGetLastError();
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || a.splits == 1 ? e : launch_cache_join(a, s);
 }
 
 template <int KIND>
-hipError_t launch_width(const CacheAttnArgs &a, hipStream_t s) {
+hipError_t launch_width(const CacheAttnArgs &a, long tiles, hipStream_t s) {
   switch (a.c.dh) {
-    case 64: return launch<KIND, 64>(a, s);
-    case 128: return launch<KIND, 128>(a, s);
-    case 256: return launch<KIND, 256>(a, s);
-    default: return launch<KIND, 512>(a, s);
+    case 64: return launch<KIND, 64>(a, tiles, s);
+    case 128: return launch<KIND, 128>(a, tiles, s);
+    case 256: return launch<KIND, 256>(a, tiles, s);
+    default: return launch<KIND, 512>(a, tiles, s);
   }
 }
 
 }  // namespace
 
-hipError_t launch_cache_prompt(const CacheAttnArgs &a, hipStream_t s) {
-  if (a.c.kind == CACHE_Q4) return launch_width<CACHE_Q4>(a, s);
-  return a.c.kind == CACHE_F16 ? launch_width<CACHE_F16>(a, s) : launch_width<CACHE_BF16>(a, s);
+hipError_t launch_cache_prompt(CacheAttnArgs a, long tiles, hipStream_t s) {
+  if (a.c.kind == CACHE_Q4) return launch_width<CACHE_Q4>(a, tiles, s);
+  return a.c.kind == CACHE_F16 ? launch_width<CACHE_F16>(a, tiles, s) : launch_width<CACHE_BF16>(a, tiles, s);
 }
 
 }  // namespace nt

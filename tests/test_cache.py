@@ -226,6 +226,34 @@ def test_prompts(torch, nt, kind, io, heads, width, page):
     f.cache.check()
 
 
+@pytest.mark.parametrize("kind,io", [("f16", "f32"), ("bf16", "bf16"), ("q4", "f16")])
+@pytest.mark.parametrize("new", [[2, 1, 0], [9, 16, 3], [17, 5, 16], [40, 0, 33], [130, 64, 1]])
+@pytest.mark.parametrize("heads,width", [((8, 2), 128), ((1, 1), 512), ((2, 2), 64)])
+def test_new_tokens_over_many_keys(torch, nt, kind, io, new, heads, width):
+    """Rows of several tokens whose keys are shared by workgroups: both kernels, and rows of sequences that are much shorter."""
+    f = Filled(torch, nt, kind, io, [5000, 70, 1], heads, width, 64, seed=sum(new), spare=20)
+    first, r = ints(torch, rows_of(new)), rows_of(new)
+    f.cache.reserve(3, first=first)
+    k, v, q = f.random(sum(new), heads[1]), f.random(sum(new), heads[1]), f.random(sum(new), heads[0])
+    hk, hv = held(torch, kind, k), held(torch, kind, v)
+    for i in range(3):
+        f.k[0][i], f.v[0][i] = np.concatenate([f.k[0][i], hk[r[i]:r[i + 1]]]), np.concatenate([f.v[0][i], hv[r[i]:r[i + 1]]])
+    for window, sinks in [(0, 0), (1500, 7)]:
+        out = torch.full((sum(new) + 1, heads[0], width), 5.0, dtype=types(torch)[io], device="cuda")
+        f.cache.attend(q, out[:-1], 3, first=first, k=k, v=v, max_new=max(new), window=window, sinks=sinks)
+        want, tol = f.expect(q, new, range(3), window, sinks)
+        compare(out[:-1], want, tol)
+        assert (out[-1] == 5).all()
+    # a value that is no number, seen by the later half of the longest's rows: no trace in the earlier ones
+    if new[0] > 1 and kind != "q4":
+        half, plain = new[0] // 2, out.clone()
+        v[half] = float("inf")
+        f.cache.attend(q, out[:-1], 3, first=first, k=k, v=v, max_new=max(new), window=1500, sinks=7)
+        assert torch.equal(out[:half], plain[:half]) and torch.equal(out[new[0]:], plain[new[0]:])
+        assert not torch.isfinite(out[half:new[0]]).any()
+    f.cache.check()
+
+
 @pytest.mark.parametrize("kind,io", [("f16", "f16"), ("bf16", "bf16"), ("q4", "f16")])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 def test_unseen_values_have_no_influence(torch, nt, kind, io, bad):

@@ -46,7 +46,7 @@ print(json.dumps((bad, good, null)))
     for kind, width, page, rc, size in good:
         token = 2 * 2 * (width * 2 if kind < 3 else width // 2 + width // 32)   # two heads, keys and values
         pool = 2 * 8 * page * token                                            # two layers of eight pages
-        split = min(8 << 20, 4 * 4 * 64 * (width + 2)) * 4                       # four sequences, four query heads, 64 shares
+        split = min(16 << 20, max(4 * 4 * 64 * (width + 2), pool // 4)) // 4 * 16  # four sequences, four query heads, 64 shares; or the pool
         assert rc == 0 and pool + split <= size <= pool + split + 32768, (kind, width, page, size - pool - split)
     assert null == [-1, -1, -1, -1, -1, -1, -1, 0]
 
