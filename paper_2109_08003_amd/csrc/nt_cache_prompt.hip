@@ -174,12 +174,16 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
   };
 
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  F ones;
+#pragma unroll
+  for (int d = 0; d < 8; d++) ones[d] = (E)1.f;
   f32x4 o[NQ][NV];
-  float top[NQ], sum[NQ];
+  float top[NQ];
+  f32x4 sum[NQ];  // of the weights as they are multiplied, in every row of a product with ones: a weight's rounding leaves a row of few keys exact
 #pragma unroll
   for (int k = 0; k < NQ; k++) {
     top[k] = kLowest;
-    sum[k] = 0.f;
+    sum[k] = zero;
 #pragma unroll
     for (int n = 0; n < NV; n++) o[k][n] = zero;
   }
@@ -289,15 +293,11 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
           for (int n = 0; n < NV; n++) o[k][n] *= shrink;
           weigh();
         }
-        float add = 0.f;
 #pragma unroll
-        for (int d = 0; d < 8; d++) {
-          const float x = __builtin_amdgcn_exp2f(z[d]);
-          add += x;
-          p[k][d] = (E)x;
-        }
-        sum[k] += add;
+        for (int d = 0; d < 8; d++) p[k][d] = (E)__builtin_amdgcn_exp2f(z[d]);
       }
+#pragma unroll
+      for (int k = 0; k < NQ; k++) sum[k] = mma(ones, p[k], sum[k]);
 #pragma unroll
       for (int n = 0; n < NV; n++) {
         const F vf = values[n * 64];
@@ -313,8 +313,7 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
 #pragma unroll
   for (int k = 0; k < NQ; k++) {
     const int row = wave_row + k * 16 + col;
-    float l = wave_pair16(sum[k], sum[k], WaveAdd{});
-    l = wave_pair32(l, l, WaveAdd{});
+    const float l = sum[k][0];
     if (row >= R) continue;
     if (w.shares > 1) {
       const long r = part0 + row - rt * ROWS;
