@@ -73,12 +73,12 @@ struct CacheAttnArgs {
   CacheView c;
   CacheRows r;
   int32_t layer, type, out_type, q_heads, group;  // group: query heads per key/value head
-  const void *q;
+  const void *q, *k, *v;  // k, v (single tokens): written to the cache first, or null
   void *out;
-  long ld_q, ld_out, lo_offset;
+  long ld_q, ld_kv, ld_out, lo_offset;
   float scale;
   int32_t window, sinks;
-  int32_t vec, vec_out;  // query rows, output rows are 16-byte aligned
+  int32_t vec, vec_kv, vec_out;  // rows are 16-byte aligned
   float *part;           // [share][row][dh], behind them {maximum, sum} [share][row]
   long part_floats;
   // set by the launchers: tiles of query rows of a sequence and their rows, workgroups that share their keys, tiles of keys that
@@ -92,6 +92,7 @@ constexpr long kPartFloats = 16l << 20;  // what the shares of a call leave for 
 hipError_t launch_cache_token(CacheAttnArgs a, long tiles, hipStream_t s);
 // Tiles of 128 or 192 query rows, likewise
 hipError_t launch_cache_prompt(CacheAttnArgs a, long tiles, hipStream_t s);
+hipError_t prepare_cache_prompt(int kind, int dh);  // once on a device before the first: its LDS
 hipError_t launch_cache_join(const CacheAttnArgs &a, hipStream_t s);  // what the shares of either have left
 
 #ifdef __HIPCC__
@@ -132,6 +133,13 @@ __device__ __forceinline__ void io_store(void *p, int type, long i, long lo, flo
   }
 }
 
+// x as bits of the cache's 16-bit type
+template <int KIND>
+__device__ __forceinline__ uint32_t half_bits(float x) {
+  if constexpr (KIND == CACHE_F16) return __builtin_bit_cast(unsigned short, (_Float16)x);
+  else return __builtin_bit_cast(unsigned short, (__bf16)x);
+}
+
 // Places within a tile of a token and a dim: 16 bits (element) and 4 bits (nibble of the keys' or values' codes)
 __device__ __forceinline__ int key_lane(int tok, int dim) { return ((dim >> 3) & 3) * 16 + (tok >> 3) * 4 + (tok & 3); }
 __device__ __forceinline__ int key_elem(int tok, int dim, int dh) {
@@ -158,6 +166,25 @@ __device__ __forceinline__ int q4_code(float x, float s) {
   const float a = fabsf(x);
   const int c = (a > 0.25f * s) + (a >= 0.75f * s) + (a > 1.25f * s) + (a >= 1.75f * s) + (a > 2.5f * s) + (a >= 3.5f * s) + (a > 5.f * s);
   return c | (x < 0.f ? 8 : 0);
+}
+// Eight values of a token, a quarter of a block whose other quarters the lanes ^ 1, ^ 2, ^ 3 have: scale byte and codes
+__device__ __forceinline__ int q4_round(const float (&x)[8], uint32_t &codes) {
+  float top = 0.f;
+  bool nan = false;
+#pragma unroll
+  for (int j = 0; j < 8; j++) top = fmaxf(top, fabsf(x[j])), nan |= x[j] != x[j];
+  if (nan) top = __builtin_nanf("");
+#pragma unroll
+  for (int m = 1; m < 4; m *= 2) {
+    const float o = __shfl_xor(top, m, 64);
+    top = top != top || o != o ? __builtin_nanf("") : fmaxf(top, o);
+  }
+  const int b = top != top ? kQ4ScaleNan : q4_scale_byte(top);
+  const float s = q4_scale(b);
+  codes = 0;
+#pragma unroll
+  for (int j = 0; j < 8; j++) codes |= (uint32_t)q4_code(x[j], s) << (4 * j);
+  return b;
 }
 __device__ __forceinline__ float q4_magnitude(int c) {  // 0, .5, 1, 1.5, 2, 3, 4, 6
   const int e = (c >> 1) & 3, m = c & 1;

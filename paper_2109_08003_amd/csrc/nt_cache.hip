@@ -523,22 +523,8 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteArgs a) {
       float val[8];
       io_load8(src, a.type, (row0 + tile * kTile + tok - base) * a.ld + (long)h * dh + dim, a.vec, val);
       if constexpr (KIND == CACHE_Q4) {
-        float top = 0.f;
-        bool nan = false;
-#pragma unroll
-        for (int j = 0; j < 8; j++) top = fmaxf(top, fabsf(val[j])), nan |= val[j] != val[j];
-        if (nan) top = __builtin_nanf("");
-        // of the block: lanes ^ 1, ^ 2
-#pragma unroll
-        for (int m = 1; m < 4; m *= 2) {
-          const float o = __shfl_xor(top, m, 64);
-          top = top != top || o != o ? __builtin_nanf("") : fmaxf(top, o);
-        }
-        const int b = top != top ? kQ4ScaleNan : q4_scale_byte(top);
-        const float sc = q4_scale(b);
-        uint32_t word = 0;
-#pragma unroll
-        for (int j = 0; j < 8; j++) word |= (uint32_t)q4_code(val[j], sc) << (4 * j);
+        uint32_t word;
+        const int b = q4_round(val, word);
         char *scales = at + 32 * dh;
         if (side == 0) {
           ((uint32_t *)at)[q4_key_word(tok, dim, dh)] = word;
@@ -550,14 +536,7 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteArgs a) {
       } else {
         uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-          if (KIND == CACHE_F16)
-            w[j] = (uint32_t)__builtin_bit_cast(unsigned short, (_Float16)val[2 * j]) |
-                   (uint32_t)__builtin_bit_cast(unsigned short, (_Float16)val[2 * j + 1]) << 16;
-          else
-            w[j] = (uint32_t)__builtin_bit_cast(unsigned short, (__bf16)val[2 * j]) |
-                   (uint32_t)__builtin_bit_cast(unsigned short, (__bf16)val[2 * j + 1]) << 16;
-        }
+        for (int j = 0; j < 4; j++) w[j] = half_bits<KIND>(val[2 * j]) | half_bits<KIND>(val[2 * j + 1]) << 16;
         if (side == 0) {
           *(uint4 *)((unsigned short *)at + key_elem(tok, dim, dh)) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
@@ -838,6 +817,7 @@ int nt_cache_create(const nt_cache_config *cfg, void *hip_stream, nt_cache **out
       return fail(NT_ENOMEM, "pinned allocation failed");
     }
     lay_out(c, c->mem);
+    HIP_TRY(nt::prepare_cache_prompt(cfg->kind, cfg->d_head));
     const int most = std::max(cfg->n_pages, cfg->max_seqs);
     hipLaunchKernelGGL(nt::cache_clear_kernel, dim3((most + 255) / 256), dim3(256), 0, as_stream(hip_stream), c->v);
     HIP_TRY(hipGetLastError());
@@ -1006,7 +986,9 @@ hipError_t nt::cache_attend(nt_cache *c, const nt_attend_args &a, int out_type, 
   const nt_cache_config &g = c->cfg;
   CacheAttnArgs k{};
   k.c = c->v; k.r = CacheRows{a.n, a.max_new, a.d_seq, a.d_first};
-  if (a.k) {
+  if (a.k && a.max_new == 1) {  // part of the attention's launch
+    k.k = a.k; k.v = a.v; k.ld_kv = a.ld_kv; k.vec_kv = aligned(a.k, a.ld_kv, a.type) && aligned(a.v, a.ld_kv, a.type);
+  } else if (a.k) {
     const hipError_t e = cache_write(c, a.layer, k.r, a.k, a.v, a.ld_kv, a.type, s);
     if (e != hipSuccess) return e;
   }

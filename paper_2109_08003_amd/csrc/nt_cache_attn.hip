@@ -19,6 +19,39 @@ constexpr int kRows = 8, kWaves = 4, kFill = 1024;
 // wave would leave one wave to a SIMD.  Their parts of the scores are added through the LDS.
 constexpr int parts_of(int dh) { return dh > 128 ? dh / 128 : 1; }
 
+// One token's key and value in a tile of a head: eight dims to a thread.  Workgroups of the same head (more than eight query heads)
+// may do the same at the same time: they write what the others write, and what else is in a word stays as it is.
+template <int KIND, int DH>
+__device__ void write_token(char *tile, int tok, const CacheAttnArgs &a, long row, int tid) {
+  const int side = tid / (DH / 8), dim = tid % (DH / 8) * 8;
+  if (side > 1) return;
+  float x[8];
+  io_load8(side ? a.v : a.k, a.type, row + dim, a.vec_kv, x);
+  if constexpr (KIND == CACHE_Q4) {
+    uint32_t codes;
+    const int scale = q4_round(x, codes);
+    uint32_t *words = (uint32_t *)(tile + 16 * DH);
+    if (side == 0) {
+      ((uint32_t *)tile)[q4_key_word(tok, dim, DH)] = codes;
+      if (dim % 32 == 0) tile[32 * DH + tok * (DH / 32) + dim / 32] = (char)scale;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; j++) {
+        uint32_t *to = words + q4_value_word(tok, dim + j);
+        *to = (*to & ~(15u << (4 * (tok & 7)))) | (codes >> (4 * j) & 15) << (4 * (tok & 7));
+      }
+      if (dim % 32 == 0) tile[33 * DH + dim / 32 * kTile + tok] = (char)scale;
+    }
+  } else if (side == 0) {
+    *(uint4 *)((unsigned short *)tile + key_elem(tok, dim, DH)) =
+        make_uint4(half_bits<KIND>(x[0]) | half_bits<KIND>(x[1]) << 16, half_bits<KIND>(x[2]) | half_bits<KIND>(x[3]) << 16,
+                   half_bits<KIND>(x[4]) | half_bits<KIND>(x[5]) << 16, half_bits<KIND>(x[6]) | half_bits<KIND>(x[7]) << 16);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; j++) ((unsigned short *)(tile + 64 * DH))[value_elem(tok, dim + j)] = (unsigned short)half_bits<KIND>(x[j]);
+  }
+}
+
 // ONE: every sequence has one new token, so the rows of a workgroup see the same keys
 template <int KIND, int DH, bool ONE>
 __global__ __launch_bounds__(256, (ONE ? 2 : 1)) void cache_token_kernel(CacheAttnArgs a) {
@@ -41,6 +74,18 @@ __global__ __launch_bounds__(256, (ONE ? 2 : 1)) void cache_token_kernel(CacheAt
   if (rt * kRows >= w.R || split >= w.shares) return;
   const int t1 = min((split + 1) * w.per, w.tiles);
 
+  if (ONE && a.k && split == w.shares - 1) {  // the newest token's key and value, to the tile that this workgroup has
+    const bool given = w.known && w.m == 1 && c.slot[w.s] == i && c.base[w.s] == w.len - 1;
+    if (given) {
+      const int tile = w.first / kTile, page = c.table[(long)w.s * c.width + (tile >> (c.page_shift - 5))];
+      if (page >= 0)
+        write_token<KIND, DH>(c.pool + cache_tile_offset(c, a.layer, page, h, tile & ((1 << (c.page_shift - 5)) - 1), cache_tile_bytes(KIND, DH)),
+                              w.first % kTile, a, w.row0 * a.ld_kv + (long)h * DH, tid);
+    } else if (h == 0 && rt == 0 && tid == 0) {
+      atomicOr(c.flags, 1);
+    }
+    __syncthreads();
+  }
   // the queries: heads of the group in columns 0 .. 7, their tails in 8 .. 15.  A power of two brings the largest of each to
   // 1 .. 2: no overflow in fp16, and tails with all their bits.
   for (int x = tid; x < kRows * DH / 8; x += 256) {
@@ -230,8 +275,8 @@ __global__ __launch_bounds__(256, (ONE ? 2 : 1)) void cache_token_kernel(CacheAt
 template <int DH>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
   __shared__ float lds_f[kRows][kMaxSplits], lds_l[kRows];
-  const int tid = threadIdx.x, lane = tid & 63, chunks = (a.tile_rows + kRows - 1) / kRows, group = blockIdx.x / chunks;
-  const int h = group % a.c.heads, rt = group / a.c.heads % a.row_tiles, i = group / a.c.heads / a.row_tiles, r0 = blockIdx.x % chunks * kRows;
+  const int tid = threadIdx.x, lane = tid & 63, group = blockIdx.x;
+  const int h = group % a.c.heads, rt = group / a.c.heads % a.row_tiles, i = group / a.c.heads / a.row_tiles, r0 = blockIdx.y * kRows;
   const Share w(a, i, rt, a.tile_rows);
   const int first = rt * a.tile_rows + r0, rows = min(min(w.R - first, kRows), a.tile_rows - r0);
   if (rows <= 0 || w.shares == 1) return;
@@ -247,20 +292,31 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
   for (int x = tid; x < rows * DH / 4; x += 256) {
     const int r = x / (DH / 4), d = x % (DH / 4) * 4;
     const f32x4 *from = (const f32x4 *)(a.part + (at + r) * DH + d);
+    const int step = a.part_rows * (DH / 4);
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int k = 0; k < w.shares; k++) y += lds_f[r][k] * from[(long)k * a.part_rows * DH / 4];
+    for (int k0 = 0; k0 < w.shares; k0 += 8) {  // eight loads under way
+      f32x4 v[8];
 #pragma unroll
-    for (int k = 0; k < 4; k++) store_row(a, w, h, first + r, d + k, DH, y[k], lds_l[r]);
+      for (int k = 0; k < 8; k++) v[k] = from[(long)min(k0 + k, w.shares - 1) * step];
+#pragma unroll
+      for (int k = 0; k < 8; k++)
+        if (k0 + k < w.shares) y += lds_f[r][k0 + k] * v[k];
+    }
+    const float l = lds_l[r];
+    const int row = first + r;
+    const long o = (w.row0 + row / a.group) * a.ld_out + (long)(h * a.group + row % a.group) * DH + d;
+#pragma unroll
+    for (int k = 0; k < 4; k++) io_store(a.out, a.out_type, o + k, a.lo_offset, l == 0.f ? 0.f : y[k] / l);
   }
 }
 
 template <int KIND, int DH>
 hipError_t launch(CacheAttnArgs a, long tiles, hipStream_t s) {
   // Shares of the keys.  Up to 1,024 workgroups, four to a CU, as many as have a turn each; beyond that as many as have kTurns, so that
-  // the longest sequences do not run on when the others are done: 64 sequences of 500 to 16,000 tokens, 8 heads, 235 us with
-  // two shares and 218 with 15; 256 in 4 bits 391 with one and 291 with 7.  Turns 2 / 4 / 8 / 16: 225 / 220 / 218 / 221, 304 / 300 / 291 / 283.
-  constexpr int kTurns = 8;
+  // the longest sequences do not run on when the others are done: 64 sequences of 500 to 16,000 tokens, 8 heads, 235 us with two
+  // shares and 218 with 15 (turns 2 / 4 / 8 / 16: 225 / 220 / 218 / 221); 256 in 4 bits, whose turns are shorter, 391 with one, 298
+  // with 15 and 287 with 7.
+  constexpr int kTurns = KIND == CACHE_Q4 ? 16 : 8;
   const long groups = (long)a.c.heads * a.row_tiles * a.r.n, at_once = kWaves / parts_of(DH);
   a.tile_rows = kRows;
   a.part_rows = (int)std::min<long>(kRows, (long)a.r.max_new * a.group);
@@ -289,7 +345,7 @@ hipError_t launch_width(const CacheAttnArgs &a, long tiles, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_cache_join(const CacheAttnArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)((long)a.r.n * a.c.heads * a.row_tiles * ((a.tile_rows + kRows - 1) / kRows))), block(256);
+  const dim3 grid((unsigned)((long)a.r.n * a.c.heads * a.row_tiles), (unsigned)((a.part_rows + kRows - 1) / kRows)), block(256);
   switch (a.c.dh) {
     case 64: hipLaunchKernelGGL(cache_join_kernel<64>, grid, block, 0, s, a); break;
     case 128: hipLaunchKernelGGL(cache_join_kernel<128>, grid, block, 0, s, a); break;

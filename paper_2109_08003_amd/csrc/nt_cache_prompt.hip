@@ -1,7 +1,7 @@
 // Attention of many rows over a paged cache: prompts.
 //
 // A workgroup has a tile of query rows of one key/value head (rows: token, then head of the group) and walks the keys that they
-// see, a stage of tiles at a time: all its waves take part in bringing the next stage to the LDS (16-bit tiles as they are, by loads
+// see, tile by tile: all its waves take part in bringing the next one to the LDS (16-bit tiles as they are, by loads
 // that go there directly; 4-bit ones rounded back to fp16 once for all waves) while each computes on the present one for its own
 // NQ x 16 rows, with the running maximum and sum of the softmax in registers.  As in the kernel for few rows, scores are S^T = K Q^T
 // and weights enter O^T = V^T P^T from the registers they are made in.
@@ -15,13 +15,16 @@ namespace {
 
 constexpr long kFill = 512;  // workgroups that the chip holds at once
 
-// Rows of a wave in tiles of 16, waves, tiles of keys in a stage.  Accumulators, queries, scores and weights of a wave are
-// NQ (DH / 4 + DH / 8 + 12) registers, 256 for two waves per SIMD; a fragment read from the LDS serves NQ products of 16 clocks,
-// and four SIMDs can read one in 32.
-template <int DH> struct PromptShape { static constexpr int NQ = 1, NW = 8, ST = 1; };
-template <> struct PromptShape<64> { static constexpr int NQ = 2, NW = 4, ST = 1; };
-template <> struct PromptShape<128> { static constexpr int NQ = 3, NW = 4, ST = 1; };
-template <> struct PromptShape<256> { static constexpr int NQ = 2, NW = 4, ST = 1; };
+// Rows of a wave in tiles of 16, and waves.  Accumulators, queries, scores and weights of a wave are about
+// NQ (DH / 4 + DH / 8 + 16) registers, and 256 let two waves share a SIMD; a fragment read from the LDS serves NQ products of 16
+// clocks, and four SIMDs can read one in 32.  Two prompts of 6,000 tokens, TFLOP/s: 32 / 8 heads of 64 with NQ 2 / 3 / 4 619 / 645 /
+// 594 (but 32 prompts of 1,000 with 8 heads 321 / 311 / 257); of 128, 8,200 tokens, 2 / 3 710 / 950; 16 / 4 of 256 with 2 x 4 / 2 x 8 /
+// 1 x 8 877 / 865 / 717, in 4 bits, whose codes on the way take registers of each wave, 432 / 706 / 617; 8 / 2 of 512 with 1 x 8 /
+// 1 x 4 690 / 432, in 4 bits 459 / 164.
+template <int KIND, int DH> struct PromptShape { static constexpr int NQ = 1, NW = 8; };
+template <int KIND> struct PromptShape<KIND, 64> { static constexpr int NQ = 2, NW = 4; };
+template <int KIND> struct PromptShape<KIND, 128> { static constexpr int NQ = 3, NW = 4; };
+template <int KIND> struct PromptShape<KIND, 256> { static constexpr int NQ = 2, NW = KIND == CACHE_Q4 ? 8 : 4; };
 
 // 0xFFFF in the halves of w that are infinities or NaN: their exponent is all ones, and one more carries into the sign
 template <typename E>
@@ -32,12 +35,12 @@ __device__ __forceinline__ uint32_t no_numbers(uint32_t w) {
 }
 
 template <int KIND, int DH>
-__global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_kernel(CacheAttnArgs a, int spread) {
+__global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_prompt_kernel(CacheAttnArgs a, int spread) {
   typedef typename FragType<KIND>::type F;
   typedef typename FragType<KIND>::elem E;
-  constexpr int NQ = PromptShape<DH>::NQ, NW = PromptShape<DH>::NW, ST = PromptShape<DH>::ST;
+  constexpr int NQ = PromptShape<KIND, DH>::NQ, NW = PromptShape<KIND, DH>::NW;
   constexpr int NC = DH / 32, NV = DH / 16, TB = 128 * DH, ROWS = NW * NQ * 16;
-  extern __shared__ __align__(1024) char lds[];  // [2][ST][TB], before that the queries
+  extern __shared__ __align__(1024) char lds[];  // [2][TB], before that the queries
   const CacheView &c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g4 = lane >> 4, G = a.group;
   // row tiles of a head's sequence, and their shares, follow one another on one of the eight dies, whose cache they share; long ones
@@ -51,7 +54,7 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
   const long row0 = w.row0;
   if ((!w.known || w.m < 0 || w.m > a.r.max_new || w.m > w.len) && h == 0 && rt == 0 && split == 0 && tid == 0) atomicOr(c.flags, 1);
   if (rt * ROWS >= R || split >= w.shares) return;
-  const int t0 = split * w.per, tiles = min(t0 + w.per, w.tiles), stages = (max(tiles - t0, 0) + ST - 1) / ST;
+  const int t0 = split * w.per, t1 = min(t0 + w.per, w.tiles);
   auto tile_of = [&](int t) { return t < w.sink_tiles ? t : w.window_tile + t - w.sink_tiles; };
 
   // queries: rounded to the cache's type in the LDS, in the order in which the waves read them back.  A power of two brings the
@@ -98,36 +101,27 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
   const int32_t *table = c.table + (long)s * c.width;
   const char *layer = c.pool + a.layer * c.layer_bytes;
   constexpr int kBytes = KIND == CACHE_Q4 ? 34 * DH : TB;
-  auto page_of = [&](int t) { return t < tiles ? table[tile_of(t) >> sub_bits] : -1; };
+  auto page_of = [&](int t) { return t < t1 ? table[tile_of(t) >> sub_bits] : -1; };
   auto address = [&](int t, int page) {
     return layer + page * c.page_bytes + (long)((h << sub_bits) + (tile_of(t) & ((1 << sub_bits) - 1))) * kBytes;
   };
 
   // pieces of a 4-bit tile that a wave brings: 16 bytes a lane, four fragments
-  constexpr int PIECES = DH / 32, MINE = KIND == CACHE_Q4 ? (ST * PIECES + NW - 1) / NW : 1;
+  constexpr int PIECES = DH / 32, MINE = KIND == CACHE_Q4 ? (PIECES + NW - 1) / NW : 1;
   uint4 code[MINE];
   uint32_t sc[MINE][4];
-  auto fetch = [&](int stage, const int (&page)[ST], int buf) {
-#pragma unroll
-    for (int x = 0; x < ST; x++) {
-      if (page[x] < 0) continue;
-      const char *at = address(t0 + stage * ST + x, page[x]);
-      if constexpr (KIND != CACHE_Q4) {
-        for (int k = wave; k < TB / 1024; k += NW)
-          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(at + k * 1024 + lane * 16),
-                                           (__attribute__((address_space(3))) void *)(lds + (buf * ST + x) * TB + k * 1024), 16, 0, 0);
-      }
-    }
-    if constexpr (KIND == CACHE_Q4) {
+  auto fetch = [&](int t, int page, int buf) {
+    if (page < 0) return;
+    const char *at = address(t, page);
+    if constexpr (KIND != CACHE_Q4) {
+      for (int k = wave; k < TB / 1024; k += NW)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(at + k * 1024 + lane * 16),
+                                         (__attribute__((address_space(3))) void *)(lds + buf * TB + k * 1024), 16, 0, 0);
+    } else {
 #pragma unroll
       for (int y = 0; y < MINE; y++) {
-        const int piece = wave + y * NW, x = piece / PIECES, p = piece % PIECES;
-        int pg = -1;
-#pragma unroll
-        for (int z = 0; z < ST; z++)
-          if (x == z) pg = page[z];
-        if (pg < 0) continue;
-        const char *at = address(t0 + stage * ST + x, pg);
+        const int p = wave + y * NW;
+        if (p >= PIECES) continue;
         code[y] = *(const uint4 *)(at + p * 1024 + lane * 16);
         if (p < PIECES / 2) {  // keys: words 4 p .. 4 p + 3
           const int tok = 8 * (col >> 2) + (col & 3);
@@ -147,13 +141,14 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
       }
     }
   };
-  auto place = [&](uint32_t there, int buf) {  // 4 bits: what fetch left in registers
+  auto place = [&](int page, int buf) {  // 4 bits: what fetch left in registers
     if constexpr (KIND == CACHE_Q4) {
+      if (page < 0) return;
 #pragma unroll
       for (int y = 0; y < MINE; y++) {
-        const int piece = wave + y * NW, x = piece / PIECES, p = piece % PIECES;
-        if (!(there >> x & 1)) continue;
-        char *to = lds + (buf * ST + x) * TB + p * 4096 + lane * 16;
+        const int p = wave + y * NW;
+        if (p >= PIECES) continue;
+        char *to = lds + buf * TB + p * 4096 + lane * 16;
 #pragma unroll
         for (int w = 0; w < 4; w++) {
           f16x2 v[4];
@@ -188,23 +183,9 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
     for (int n = 0; n < NV; n++) o[k][n] = zero;
   }
 
-  int next[ST];
-  uint32_t present = 0, present_next = 0;  // bit x: tile x of the stage has a page
-  auto look_up = [&](int stage) {
-#pragma unroll
-    for (int x = 0; x < ST; x++) next[x] = page_of(t0 + stage * ST + x);
-  };
-  auto mask_of = [&]() {
-    uint32_t b = 0;
-#pragma unroll
-    for (int x = 0; x < ST; x++) b |= (next[x] >= 0 ? 1u : 0u) << x;
-    return b;
-  };
-  look_up(0);
-  present = mask_of();
-  fetch(0, next, 0);
-  place(present, 0);
-  look_up(1);
+  int page = page_of(t0), next = page_of(t0 + 1);
+  fetch(t0, page, 0);
+  place(page, 0);
   // whether all rows of the workgroup see all keys of a tile
   auto seen_by_all = [&](int j0) { return j0 + kTile - 1 <= p_min && (a.window == 0 || j0 >= p_max - a.window + 1 || j0 + kTile <= a.sinks); };
   // Where they do not, the values of keys that none sees, and those that are no numbers, become zero in the LDS before the product.
@@ -225,26 +206,17 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
     }
   };
   __syncthreads();
-  for (int stage = 0; stage < stages; stage++) {
-    const int buf = stage & 1;
-    present_next = mask_of();
-    fetch(stage + 1, next, buf ^ 1);
-    look_up(stage + 2);
-    bool cleaned = false;
-    for (int x = 0; x < ST; x++) {
-      const int j0 = tile_of(t0 + stage * ST + x) * kTile;
-      if (!(present >> x & 1) || t0 + stage * ST + x >= tiles || seen_by_all(j0)) continue;
-      clean(j0, lds + (buf * ST + x) * TB);
-      cleaned = true;
+  for (int t = t0; t < t1; t++) {
+    const int buf = (t - t0) & 1, j0 = tile_of(t) * kTile, after = page_of(t + 2);
+    fetch(t + 1, next, buf ^ 1);
+    if (page >= 0 && !seen_by_all(j0)) {
+      clean(j0, lds + buf * TB);
+      __syncthreads();
     }
-    if (cleaned) __syncthreads();
-#pragma unroll 1
-    for (int x = 0; x < ST; x++) {
-      const int j0 = tile_of(t0 + stage * ST + x) * kTile;
-      // nothing for this wave
-      if (!(present >> x & 1) || j0 > w_max || (j0 + kTile <= w_low && j0 >= a.sinks)) continue;
+    // unless there is nothing for this wave
+    if (page >= 0 && j0 <= w_max && (j0 + kTile > w_low || j0 < a.sinks)) {
       const bool all_seen = j0 + kTile - 1 <= w_min && (a.window == 0 || j0 >= w_max - a.window + 1 || j0 + kTile <= a.sinks);
-      const F *keys = (const F *)(lds + (buf * ST + x) * TB) + lane, *values = keys + 4 * DH;
+      const F *keys = (const F *)(lds + buf * TB) + lane, *values = keys + 4 * DH;
       f32x4 y[NQ][2];
 #pragma unroll
       for (int k = 0; k < NQ; k++) y[k][0] = y[k][1] = zero;
@@ -305,8 +277,9 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
         for (int k = 0; k < NQ; k++) o[k][n] = mma(vf, p[k], o[k][n]);
       }
     }
-    place(present_next, buf ^ 1);
-    present = present_next;
+    place(next, buf ^ 1);
+    page = next;
+    next = after;
     __syncthreads();
   }
   const long part0 = ((long)((i * a.row_tiles + rt) * c.heads + h) * a.splits + split) * a.part_rows;
@@ -348,7 +321,7 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
   }
   if (!lds_strange) return;
   // The infinities and NaN that were left out reach the rows that see them: a lane corrects what it has stored.
-  for (int t = t0; t < tiles; t++) {
+  for (int t = t0; t < t1; t++) {
     const int pg = page_of(t), j0 = tile_of(t) * kTile;
     if (pg < 0 || seen_by_all(j0)) continue;
     const char *at = address(t, pg);
@@ -378,12 +351,14 @@ __global__ __launch_bounds__((PromptShape<DH>::NW * 64), 2) void cache_prompt_ke
 }
 
 template <int KIND, int DH>
+struct PromptLaunch {
+  static constexpr int kRows = PromptShape<KIND, DH>::NW * PromptShape<KIND, DH>::NQ * 16, kTiles = 2 * 128 * DH, kQueries = kRows * DH * 2;
+  static constexpr int kLds = kTiles > kQueries ? kTiles : kQueries;  // first the queries, then the tiles
+};
+
+template <int KIND, int DH>
 hipError_t launch(CacheAttnArgs a, long tiles, hipStream_t s) {
-  typedef PromptShape<DH> P;
-  constexpr int kRows = P::NW * P::NQ * 16, kStages = 2 * P::ST * 128 * DH, kQueries = kRows * DH * 2;
-  constexpr int kLds = kStages > kQueries ? kStages : kQueries;  // first the queries, then the stages
-  static const hipError_t limit = hipFuncSetAttribute((const void *)cache_prompt_kernel<KIND, DH>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-  if (limit != hipSuccess) return limit;
+  constexpr int kRows = PromptLaunch<KIND, DH>::kRows;
   a.row_tiles = (int)(((long)a.r.max_new * a.group + kRows - 1) / kRows);
   const long units = (long)a.r.n * a.c.heads, groups = units * a.row_tiles;
   // Shares of the keys where there are fewer workgroups than the chip holds, two to a CU, of kTurns tiles at least.
@@ -396,9 +371,24 @@ hipError_t launch(CacheAttnArgs a, long tiles, hipStream_t s) {
   // spread over the dies by unit where that leaves none idle
   const int spread = units % 8 == 0 || units >= 64;
   const long blocks = (spread ? (units + 7) / 8 * 8 : units) * a.row_tiles * a.splits;
-  hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH>), dim3((unsigned)blocks), dim3(P::NW * 64), kLds, s, a, spread);
+  hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH>), dim3((unsigned)blocks), dim3(PromptShape<KIND, DH>::NW * 64),
+                     (PromptLaunch<KIND, DH>::kLds), s, a, spread);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || a.splits == 1 ? e : launch_cache_join(a, s);
+}
+
+template <int KIND, int DH>
+hipError_t prepare() {
+  return hipFuncSetAttribute((const void *)cache_prompt_kernel<KIND, DH>, hipFuncAttributeMaxDynamicSharedMemorySize, PromptLaunch<KIND, DH>::kLds);
+}
+template <int KIND>
+hipError_t prepare_width(int dh) {
+  switch (dh) {
+    case 64: return prepare<KIND, 64>();
+    case 128: return prepare<KIND, 128>();
+    case 256: return prepare<KIND, 256>();
+    default: return prepare<KIND, 512>();
+  }
 }
 
 template <int KIND>
@@ -413,6 +403,9 @@ hipError_t launch_width(const CacheAttnArgs &a, long tiles, hipStream_t s) {
 
 }  // namespace
 
+hipError_t prepare_cache_prompt(int kind, int dh) {
+  return kind == CACHE_Q4 ? prepare_width<CACHE_Q4>(dh) : kind == CACHE_F16 ? prepare_width<CACHE_F16>(dh) : prepare_width<CACHE_BF16>(dh);
+}
 hipError_t launch_cache_prompt(CacheAttnArgs a, long tiles, hipStream_t s) {
   if (a.c.kind == CACHE_Q4) return launch_width<CACHE_Q4>(a, tiles, s);
   return a.c.kind == CACHE_F16 ? launch_width<CACHE_F16>(a, tiles, s) : launch_width<CACHE_BF16>(a, tiles, s);

@@ -101,7 +101,7 @@ print(json.dumps(out))
         for name, blocks in launches:
             assert 0 < blocks < 2 ** 31, (name, blocks)
         write = [b for name, b in launches if "cache_write" in name]
-        assert write == [((new + 30) // 32 + 1) * 2 * n]
+        assert write == ([((new + 30) // 32 + 1) * 2 * n] if new > 1 else [])  # a single token is written by the attention
 
 
 def test_models_with_a_paged_self_cache(host):  # noqa: F811
@@ -133,7 +133,7 @@ for _ in range(2):
     stub.stub_clear()
     nt.binding._check(lib().nt_decode_greedy(model._h, 3, 5, None, out.ctypes.data, None))
     names = [n for n, b in launches()]
-    steps.append([sum(w in n for n in names) for w in ("cache_end", "cache_reserve", "cache_write", "cache_token", "dec1_kernel")])
+    steps.append([sum(w in n for n in names) for w in ("cache_end", "cache_reserve", "cache_token", "cache_join", "dec1_kernel")])
 print(json.dumps((codes, older, sizes, steps)))
 """)
     assert codes == [-1, -1, -1, -1, -1, -1, -2]
@@ -141,4 +141,4 @@ print(json.dumps((codes, older, sizes, steps)))
     positions = (6 * 2048 + 4) // 5 + 3 * 2048 + 8
     pages = positions // 32 + 2048
     assert sizes[0] == sizes[1] and sizes[0] - sizes[2] == pages * 32 * 2 * (512 * 2 - 512 // 2 - 512 // 32)
-    assert steps == [[0, 5, 10, 10, 0], [1, 5, 10, 10, 0]]
+    assert steps == [[0, 5, 10, 0, 0], [1, 5, 10, 0, 0]]
