@@ -295,8 +295,9 @@ int nt_plan_batches(const int32_t *h_lengths, int64_t N, int64_t budget, int32_t
  *   max_seqs      at most 2^20
  *   max_len       longest sequence, at most 2^24
  *
- * The calls below only enqueue kernels on hip_stream, allocate nothing and may be captured into a graph.  Calls on one
- * cache must follow one another: in one stream, or ordered by events.  All have to be made with the device current on
+ * The calls below, other than nt_cache_create, nt_cache_destroy and nt_cache_check, only enqueue kernels on hip_stream,
+ * allocate nothing and may be captured into a graph.  Calls on one cache must follow one another: in one stream, or
+ * ordered by events; outputs must not overlap inputs.  All have to be made with the device current on
  * which the cache was created.  What the host cannot see is checked on the device: a sequence id outside [0, max_seqs),
  * the second of two equal ids in a call that changes sequences, a length that does not fit.  Such an entry is skipped, its
  * sequence stays as it was, and nt_cache_check reports it; so it is where no free pages are left (entries are served in
@@ -357,7 +358,8 @@ int nt_cache_write(nt_cache *c, int32_t layer, int32_t n, const int32_t *d_seq, 
  * Keys and values that a query does not see have no influence on it, whatever they are.  Scores, weights and sums are
  * fp32; with one row per sequence the queries and weights enter the products with about twice the bits of the
  * cache's type (fp16 for 4 bits), with more they are rounded to that type.
- * Errors as above; NT_EINVAL for a wrong struct_size, a negative window or number of sinks, or only one of k and v.
+ * Errors as above; NT_EINVAL for a wrong struct_size, a negative window or number of sinks, a scale that is
+ * infinite or NaN, or only one of k and v.
  */
 typedef struct {
   uint32_t struct_size; /* sizeof(nt_attend_args), checked */

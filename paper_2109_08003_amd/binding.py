@@ -376,8 +376,9 @@ class Model:
 class Cache:
     """Owns one nt_cache: keys and values of many sequences in pages, as fp16, bf16 or 4 bits (kind "f16", "bf16", "q4").
 
-    Methods mirror the C entry points.  Values are cuda tensors of float32, float16 or bfloat16; seqs, first, lengths are contiguous
-    int32 cuda tensors.  seqs None = sequences 0 .. n - 1; first None = one row each."""
+    Methods mirror the C entry points.  Values are tensors of float32, float16 or bfloat16, seqs, first, lengths contiguous tensors of int32,
+    all on the device that was current when the cache was made.  seqs None = sequences 0 .. n - 1; first None = one row each.  One cache
+    must not be used from two threads at once."""
 
     def __init__(self, kind: str, n_layers: int, n_q_heads: int, n_kv_heads: int, d_head: int, n_pages: int, max_seqs: int, max_len: int,
                  page_tokens: int = 64, stream=None):
@@ -389,6 +390,7 @@ class Cache:
         import torch
         self._lib, self._int32, self._types = lib(), torch.int32, {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
         self._current_stream, self._scale = torch.cuda.current_stream, d_head ** -0.5
+        self._device = torch.cuda.current_device() if torch.cuda.is_available() else 0
         self._args = NtAttendArgs(C.sizeof(NtAttendArgs))
         self._args_ref = C.byref(self._args)
 
@@ -430,15 +432,15 @@ class Cache:
     def _ints(self, t, size):
         if t is None:
             return None
-        if t.dtype is not self._int32 or not t.is_cuda or not t.is_contiguous() or t.numel() < size:
-            raise TypeError(f"a contiguous int32 cuda tensor of at least {size} entries is needed")
+        if t.dtype is not self._int32 or t.get_device() != self._device or not t.is_contiguous() or t.numel() < size:
+            raise TypeError(f"a contiguous int32 tensor of at least {size} entries on the cache's device is needed")
         return t.data_ptr()
 
     def _rows(self, t, heads):
         """(rows, row stride) of a [rows, heads, d_head] tensor whose heads are dense."""
         d, shape, stride = self.config.d_head, t.shape, t.stride()
-        if len(shape) != 3 or shape[1] != heads or shape[2] != d or stride[2] != 1 or (heads > 1 and stride[1] != d) or not t.is_cuda:
-            raise TypeError(f"a cuda tensor [rows, {heads}, {d}] with dense heads is needed")
+        if len(shape) != 3 or shape[1] != heads or shape[2] != d or stride[2] != 1 or (heads > 1 and stride[1] != d) or t.get_device() != self._device:
+            raise TypeError(f"a tensor [rows, {heads}, {d}] with dense heads on the cache's device is needed")
         return shape[0], stride[0] if shape[0] > 1 else max(stride[0], heads * d)
 
     def _count(self, n, seqs):
@@ -488,17 +490,23 @@ class Cache:
         n, g = self._count(n, seqs), self.config
         shape = k.shape
         if v.shape != shape or len(shape) != 4 or shape[0] < n or shape[2] != g.n_kv_heads or shape[3] != g.d_head or not (
-                k.is_cuda and v.is_cuda and k.is_contiguous() and v.is_contiguous()):
-            raise TypeError(f"contiguous cuda tensors [{n}, max_keys, {g.n_kv_heads}, {g.d_head}] are needed")
+                k.get_device() == v.get_device() == self._device and k.is_contiguous() and v.is_contiguous()):
+            raise TypeError(f"contiguous tensors [{n}, max_keys, {g.n_kv_heads}, {g.d_head}] on the cache's device are needed")
         _check(self._lib.nt_cache_read(self._h, layer, n, self._ints(seqs, n), shape[1], k.data_ptr(), v.data_ptr(), self._type(k, v),
                                    self._stream(stream)))
 
+    @staticmethod
+    def _pairs(src, dst):
+        if src.numel() != dst.numel():
+            raise TypeError("as many sources as targets are needed")
+        return src.numel()
+
     def fork(self, src, dst, stream=None):
-        n = src.numel()
+        n = self._pairs(src, dst)
         _check(self._lib.nt_cache_fork(self._h, n, self._ints(src, n), self._ints(dst, n), self._stream(stream)))
 
     def copy(self, src, dst, stream=None):
-        n = src.numel()
+        n = self._pairs(src, dst)
         _check(self._lib.nt_cache_copy(self._h, n, self._ints(src, n), self._ints(dst, n), self._stream(stream)))
 
     def truncate(self, n: int = None, seqs=None, lengths=None, stream=None):

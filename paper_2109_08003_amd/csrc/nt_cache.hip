@@ -870,6 +870,7 @@ int nt_cache_attend(nt_cache *c, const nt_attend_args *a, void *hip_stream) {
   if (!type_known(a->type)) return fail(NT_EINVAL, "unknown type %d", a->type);
   if (a->max_new < 0 || a->max_new > g.max_len) return fail(NT_ERANGE, "max_new %d outside [0, max_len=%d]", a->max_new, g.max_len);
   if (a->window < 0 || a->sinks < 0 || a->max_keys < 0) return fail(NT_EINVAL, "negative window, sinks or max_keys");
+  if (!std::isfinite(a->scale)) return fail(NT_EINVAL, "scale is not a number");
   if (!a->d_first && a->max_new != 1) return fail(NT_EINVAL, "max_new must be 1 without d_first");
   if (!a->k != !a->v) return fail(NT_EINVAL, "one of k and v without the other");
   if (a->n == 0 || a->max_new == 0) return NT_OK;

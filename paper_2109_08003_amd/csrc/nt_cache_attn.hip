@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256, (ONE ? 2 : 1)) void cache_token_kernel(CacheAt
 #pragma unroll
     for (int k = 1; k < DH / 8; k *= 2) big = fmaxf(big, __shfl_xor(big, k, 64));
     const int e = big > 0.f && big < __builtin_inff() ? min(max(ilogbf(big), -100), 126) : 0;
-    if (d == 0) lds_scale[r] = ldexpf(fabsf(a.scale) * 1.44269504088896f, e);
+    if (d == 0) lds_scale[r] = fmaxf(ldexpf(fabsf(a.scale) * 1.44269504088896f, e), kLeastScale);
     const float down = ldexpf(a.scale < 0.f ? -1.f : 1.f, -e);
     F head, tail;
 #pragma unroll

@@ -8,6 +8,7 @@ namespace nt {
 // The running maximum of a row changes only where a score exceeds it by more than kSlack (as a logarithm of base 2): weights are up to
 // 2^8 then, which no type here minds, and most tiles rescale nothing.
 constexpr float kSlack = 8.f;
+constexpr float kLeastScale = 1e-30f;  // for a scale of 0: the minus infinity of a key that is not seen stays one
 constexpr float kLowest = -1e38f;  // maximum of no score; less than any that is a number
 
 // What a workgroup has to do: the rows of sequence i in row tile rt of `rows` rows, the tiles of keys that one of them sees (those of the sinks, then

@@ -72,7 +72,7 @@ __global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_pro
 #pragma unroll
     for (int k = 1; k < DH / 8; k *= 2) big = fmaxf(big, __shfl_xor(big, k, 64));
     const int ex = big > 0.f && big < __builtin_inff() ? min(max(ilogbf(big), -100), 126) : 0;
-    if (d == 0) lds_scale[r] = ldexpf(fabsf(a.scale) * 1.44269504088896f, ex);
+    if (d == 0) lds_scale[r] = fmaxf(ldexpf(fabsf(a.scale) * 1.44269504088896f, ex), kLeastScale);
     const float down = ldexpf(a.scale < 0.f ? -1.f : 1.f, -ex);
     F f;
 #pragma unroll

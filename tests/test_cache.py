@@ -187,6 +187,59 @@ def test_tokens_over_many_keys(torch, nt, kind, io, lens, max_keys):
     f.cache.check()
 
 
+@pytest.mark.parametrize("kind,io", [("bf16", "f32"), ("f16", "bf16"), ("bf16", "f16")])
+def test_other_pairs_of_types(torch, nt, kind, io):
+    f = Filled(torch, nt, kind, io, [1, 40, 300], (4, 2), 128, 64, seed=2)
+    q = f.random(3, 4)
+    out = torch.empty_like(q)
+    f.cache.attend(q, out, 3, window=100, sinks=3)
+    want, tol = f.expect(q, [1, 1, 1], range(3), 100, 3, tokens=True)
+    compare(out, want, tol)
+    new, first = [1, 30, 100], ints(torch, [0, 1, 31, 131])
+    f.cache.truncate(3, lengths=ints(torch, [1, 40, 300]))
+    f.cache.reserve(3, first=first)
+    k, v, q = f.random(131, 2), f.random(131, 2), f.random(131, 4)
+    hk, hv, r = held(torch, kind, k), held(torch, kind, v), rows_of(new)
+    for i in range(3):
+        f.k[0][i], f.v[0][i] = np.concatenate([f.k[0][i], hk[r[i]:r[i + 1]]]), np.concatenate([f.v[0][i], hv[r[i]:r[i + 1]]])
+    out = torch.empty_like(q)
+    f.cache.attend(q, out, 3, first=first, k=k, v=v, max_new=100)
+    want, tol = f.expect(q, new, range(3), 0, 0)
+    compare(out, want, tol)
+    f.cache.check()
+
+
+def test_negative_and_zero_scale(torch, nt):
+    for kind, new in (("f16", 1), ("q4", 1), ("f16", 70), ("bf16", 70)):
+        io = "bf16" if kind == "bf16" else "f16"
+        f = Filled(torch, nt, kind, io, [100], (4, 2), 64, 64, seed=2)
+        q = f.random(new, 4)
+        for scale in (-0.2, 0.0):
+            out = torch.empty_like(q)
+            f.cache.attend(q, out, 1, first=ints(torch, [0, new]) if new > 1 else None, max_new=new, scale=scale)
+            want, tol = f.expect(q, [new], [0], 0, 0, scale=scale, tokens=new == 1)
+            compare(out, want, tol)
+
+
+def test_one_step_of_many_sequences(torch, nt):
+    """More sequences than workgroups that share keys, ids in any order, twelve query heads to a key/value head."""
+    n = 1500
+    lens = [1 + i % 90 for i in range(n)]
+    f = Filled(torch, nt, "q4", "bf16", lens, (12, 1), 64, 32, seed=5, spare=40)  # 34 of them are 32 or 64 long: the step takes as many pages
+    order = np.random.default_rng(1).permutation(n)
+    d = ints(torch, order)
+    f.cache.reserve(seqs=d)
+    k, v, q = f.random(n, 1), f.random(n, 1), f.random(n, 12)
+    out = torch.empty_like(q)
+    f.cache.attend(q, out, seqs=d, k=k, v=v, window=60, sinks=1)
+    hk, hv = held(torch, "q4", k), held(torch, "q4", v)
+    for i, s in enumerate(order):
+        f.k[0][s], f.v[0][s] = np.concatenate([f.k[0][s], hk[i:i + 1]]), np.concatenate([f.v[0][s], hv[i:i + 1]])
+    want, tol = f.expect(q, [1] * n, order, 60, 1, tokens=True)
+    compare(out, want, tol)
+    f.cache.check()
+
+
 def test_large_and_tiny_numbers(torch, nt):
     """Queries beyond fp16 with small keys, tiny queries with large keys.  (Without the scale of 1e-3 the first kind's scores were
     sums of 64 products of about 1e6 * 3e-3 * 0.6, and fp32 sums of 1e5 decide no weight: 68 half steps of them are 0.5.)"""

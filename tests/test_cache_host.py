@@ -66,6 +66,7 @@ rcs = {
   "no keys": L.nt_cache_write(h, 0, 1, None, None, 1, None, x, 128, 0, None),
   "struct_size": attend(h, struct_size=7),
   "window": attend(h, window=-1), "sinks": attend(h, sinks=-1), "max_keys": attend(h, max_keys=-1),
+  "scale": attend(h, scale=float("nan")), "infinite scale": attend(h, scale=float("inf")),
   "q stride": attend(h, ld_q=255), "out stride": attend(h, ld_out=255), "kv stride": attend(h, k=x, v=x, ld_kv=127),
   "k alone": attend(h, k=x, ld_kv=128), "no q": attend(h, q=None), "no out": attend(h, out=None),
   "rows without d_first": attend(h, max_new=2), "attend layer": attend(h, layer=2), "attend type": attend(h, type=9), "attend n": attend(h, n=5),
@@ -142,3 +143,46 @@ print(json.dumps((codes, older, sizes, steps)))
     pages = positions // 32 + 2048
     assert sizes[0] == sizes[1] and sizes[0] - sizes[2] == pages * 32 * 2 * (512 * 2 - 512 // 2 - 512 // 32)
     assert steps == [[0, 5, 10, 0, 0], [1, 5, 10, 0, 0]]
+
+
+def test_binding_refuses_tensors_that_do_not_fit(host):  # noqa: F811
+    """Host tensors, other devices, types, shapes and strides; nothing is launched."""
+    kinds, launched = host("""
+import torch
+class Dev:  # a host tensor that says it is on a device
+    def __init__(self, t, device=0):
+        self.t, self.device = t, device
+    def get_device(self):
+        return self.device
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+c = nt.Cache("f16", 1, 4, 2, 64, 8, 4, 200, stream=Stream)
+def t(*shape, dtype=torch.float16, device=0):
+    return Dev(torch.zeros(shape, dtype=dtype), device)
+q, out, k = t(3, 4, 64), t(3, 4, 64), t(3, 2, 64)
+ids = t(3, dtype=torch.int32)
+wide = Dev(torch.zeros(3, 4, 128, dtype=torch.float16)[:, :, ::2])
+stub.stub_clear()
+def kind(f):
+    try:
+        f()
+        return "none"
+    except (TypeError, nt.NtError) as e:
+        return type(e).__name__
+s = dict(stream=Stream)
+kinds = [kind(f) for f in (
+    lambda: c.attend(torch.zeros(3, 4, 64).half(), out, 3, **s), lambda: c.attend(t(3, 4, 64, device=1), out, 3, **s),
+    lambda: c.attend(q, t(3, 4, 64, dtype=torch.float32), 3, **s), lambda: c.attend(t(3, 4, 64, dtype=torch.float64), t(3, 4, 64, dtype=torch.float64), 3, **s),
+    lambda: c.attend(t(3, 5, 64), t(3, 5, 64), 3, **s), lambda: c.attend(wide, out, 3, **s), lambda: c.attend(q, t(2, 4, 64), 3, **s),
+    lambda: c.attend(q, out, 4, **s), lambda: c.attend(q, out, **s), lambda: c.attend(q, out, 3, k=k, **s), lambda: c.attend(q, out, 3, k=k, v=t(2, 2, 64), **s),
+    lambda: c.attend(q, out, seqs=t(3, dtype=torch.int64), **s), lambda: c.attend(q, out, 3, seqs=t(2, dtype=torch.int32), **s),
+    lambda: c.attend(q, out, 3, first=ids, **s), lambda: c.write(k, t(3, 2, 64, dtype=torch.float32), 3, **s), lambda: c.write(k, k, 4, **s),
+    lambda: c.read(t(3, 9, 2, 64), t(3, 8, 2, 64), 3, **s), lambda: c.read(t(2, 9, 2, 64), t(2, 9, 2, 64), 3, **s),
+    lambda: c.fork(ids, t(2, dtype=torch.int32), **s), lambda: c.reserve(seqs=t(3, dtype=torch.int32, device=1), **s),
+    lambda: c.attend(q, out, 3, window=-1, **s), lambda: c.reserve(5, **s))]
+launched = stub.stub_n_launches()
+c.attend(q, out, 3, k=k, v=k, **s)
+print(json.dumps((kinds, (launched, stub.stub_n_launches()))))
+""")
+    assert kinds == ["TypeError"] * 20 + ["NtError"] * 2
+    assert launched[0] == 0 < launched[1]
