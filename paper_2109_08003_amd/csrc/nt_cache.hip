@@ -775,8 +775,8 @@ int become(nt_cache *c, int32_t n, const int32_t *d_src, const int32_t *d_dst, i
   if (rc || n == 0) return rc;
   if (!d_src || !d_dst) return fail(NT_EINVAL, "null argument");
   hipStream_t s = as_stream(hip_stream);
-  // 16 waves go through the table's rows as fast as a launch of their own, and a third, begin: 48 entries of one page or two 22 us
-  // for both launches against XXX for the three.
+  // A table of few rows is the planning workgroup's as well: one launch less to enqueue.  48 entries of one page or two, with the
+  // reading of what they became: 19 us of the host's time and 22 in all, 23 and 24 with the table's launches of their own.
   const int whole = (double)n * c->v.width > 4096 ? 0 : c->v.width <= 16 ? 16 : 64, tables = whole ? 0 : n;
   const int copies = nt::copy_blocks(c->v, c->cfg.n_layers, deep ? (double)n * c->v.width : n);
   hipLaunchKernelGGL(nt::cache_fork_plan_kernel, dim3(1), dim3(nt::kPlan), 0, s, c->v, n, d_src, d_dst, deep, whole, c->w);

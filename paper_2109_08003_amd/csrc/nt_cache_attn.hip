@@ -128,12 +128,15 @@ __global__ __launch_bounds__(256, (ONE ? 2 : 1)) void cache_token_kernel(CacheAt
     const char *at = address(t, page);
     kt.load(at, lane, part);
     vt.load(at, lane, part);
+  } else if (PARTS > 1) {  // a wave that has to meet the others all the same
+    kt = {};
+    vt = {};
   }
   __syncthreads();
   F q[NC];
 #pragma unroll
   for (int k = 0; k < NC; k++) q[k] = ((const F *)lds_q)[(part * NC + k) * 64 + lane];
-  const float to_log2 = lds_scale[col & 7];
+  const float to_log2 = lds_scale[col & 7], tails = col < 8 ? 0.f : 1.f;
 
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   f32x4 o[NV];
@@ -216,8 +219,7 @@ __global__ __launch_bounds__(256, (ONE ? 2 : 1)) void cache_token_kernel(CacheAt
     for (int j = 0; j < 8; j++) {
       const float x = __builtin_amdgcn_exp2f(z[j]);
       sum += x;
-      const E head = (E)x;
-      p[j] = col < 8 ? head : (E)(x - (float)head);
+      p[j] = (E)__builtin_fmaf(-(float)(E)x, tails, x);  // exact before it is rounded
     }
     bool bad = false;
     if (!ONE && !all_seen && w.p_min < w.p_max) {  // rows of different tokens: some see keys that others do not
