@@ -355,9 +355,10 @@ int nt_cache_write(nt_cache *c, int32_t layer, int32_t n, const int32_t *d_seq, 
  *              rows that are too many and is reported)
  *   max_keys   the longest of the sequences, as far as the caller knows; chooses how the work is split, nothing else.
  *              0 = max_len
- * Keys and values that a query does not see have no influence on it, whatever they are.  Scores, weights and sums are
- * fp32; with one row per sequence the queries and weights enter the products with about twice the bits of the
- * cache's type (fp16 for 4 bits), with more they are rounded to that type.
+ * Keys and values that a query does not see have no influence on it, whatever they are; infinities that it sees give
+ * infinities or NaN.  Scores, weights and sums are
+ * fp32; rows of fp32, and one row per sequence of any type, enter the products, and their weights, with about twice the
+ * bits of the cache's type (fp16 for 4 bits), several rows of fp16 or bf16 are rounded to that type.
  * Errors as above; NT_EINVAL for a wrong struct_size, a negative window or number of sinks, a scale that is
  * infinite or NaN, or only one of k and v.
  */

@@ -90,7 +90,7 @@ constexpr int kMaxSplits = 64;  // shares of one row's keys: a lane each in the 
 constexpr long kPartFloats = 16l << 20;  // what the shares of a call leave for the join, at most: 512 of 192 rows of 128, 32,000 of four
 // Queries in tiles of 8 (rows: token, then head of the group), each split over the keys, of which a row sees about `tiles` tiles.
 hipError_t launch_cache_token(CacheAttnArgs a, long tiles, hipStream_t s);
-// Tiles of 128 or 192 query rows, likewise
+// Tiles of 64 to 256 query rows, likewise
 hipError_t launch_cache_prompt(CacheAttnArgs a, long tiles, hipStream_t s);
 hipError_t prepare_cache_prompt(int kind, int dh);  // once on a device before the first: its LDS
 hipError_t launch_cache_join(const CacheAttnArgs &a, hipStream_t s);  // what the shares of either have left

@@ -172,7 +172,7 @@ __global__ __launch_bounds__(256, (ONE ? 2 : 1)) void cache_token_kernel(CacheAt
 #pragma unroll
     for (int j = 0; j < 8; j++) {
       const float x = sc[j / 4][j % 4];
-      y[j] = x + __uint_as_float(wave_dpp<0x128>(__float_as_uint(x)));  // head and tail: columns 8 apart
+      y[j] = x + eight_on(x);  // head and tail: columns 8 apart
     }
     const bool all_seen =
         page >= 0 && j0 + kTile - 1 <= w.p_min && (a.window == 0 || j0 >= w.p_max - a.window + 1 || j0 + kTile <= a.sinks);
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(256, (ONE ? 2 : 1)) void cache_token_kernel(CacheAt
   for (int n = 0; n < NV; n++) {
     f32x4 x = o[n];
 #pragma unroll
-    for (int k = 0; k < 4; k++) x[k] += __uint_as_float(wave_dpp<0x128>(__float_as_uint(x[k])));
+    for (int k = 0; k < 4; k++) x[k] = head_and_tail(x[k]);
     if (col < 8) *(f32x4 *)&lds_o[mine][col][part * DW + n * 16 + g4 * 4] = x;
   }
   __syncthreads();

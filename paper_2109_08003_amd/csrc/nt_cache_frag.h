@@ -38,6 +38,16 @@ struct Share {
   }
 };
 
+// x of the column eight on (or back): the other of a row's head and tail
+__device__ __forceinline__ float eight_on(float x) { return __uint_as_float(wave_dpp<0x128>(__float_as_uint(x))); }
+
+// Head's and tail's sums of values, in the head's column.  Where an infinity is among the values the head's is one, and the tail's
+// whatever its sign has made of it.
+__device__ __forceinline__ float head_and_tail(float x) {
+  const float y = x + eight_on(x);
+  return fabsf(x) == __builtin_inff() ? x : y;
+}
+
 // x / l, zero where no key was seen
 __device__ __forceinline__ void store_row(const CacheAttnArgs &a, const Share &w, int h, int row, int d, int dh, float x, float l) {
   if (row < w.R)

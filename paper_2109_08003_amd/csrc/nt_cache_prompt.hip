@@ -5,6 +5,9 @@
 // that go there directly; 4-bit ones rounded back to fp16 once for all waves) while each computes on the present one for its own
 // NQ x 16 rows, with the running maximum and sum of the softmax in registers.  As in the kernel for few rows, scores are S^T = K Q^T
 // and weights enter O^T = V^T P^T from the registers they are made in.
+//
+// Rows of fp16 and bf16 are rounded to the cache's type for the products, weights likewise.  Rows of fp32 (WIDE) keep about twice those
+// bits: as in the kernel for few rows, the sixteen columns of an instruction are then eight rows twice, heads and tails.
 #include <algorithm>
 #include <climits>
 
@@ -34,12 +37,12 @@ __device__ __forceinline__ uint32_t no_numbers(uint32_t w) {
   return (b << 1) - (b >> 15);
 }
 
-template <int KIND, int DH>
+template <int KIND, int DH, bool WIDE>
 __global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_prompt_kernel(CacheAttnArgs a, int spread) {
   typedef typename FragType<KIND>::type F;
   typedef typename FragType<KIND>::elem E;
   constexpr int NQ = PromptShape<KIND, DH>::NQ, NW = PromptShape<KIND, DH>::NW;
-  constexpr int NC = DH / 32, NV = DH / 16, TB = 128 * DH, ROWS = NW * NQ * 16;
+  constexpr int NC = DH / 32, NV = DH / 16, TB = 128 * DH, RT = WIDE ? 8 : 16, ROWS = NW * NQ * RT;
   extern __shared__ __align__(1024) char lds[];  // [2][TB], before that the queries
   const CacheView &c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g4 = lane >> 4, G = a.group;
@@ -74,19 +77,26 @@ __global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_pro
     const int ex = big > 0.f && big < __builtin_inff() ? min(max(ilogbf(big), -100), 126) : 0;
     if (d == 0) lds_scale[r] = fmaxf(ldexpf(fabsf(a.scale) * 1.44269504088896f, ex), kLeastScale);
     const float down = ldexpf(a.scale < 0.f ? -1.f : 1.f, -ex);
-    F f;
+    F head, tail;
 #pragma unroll
-    for (int k = 0; k < 8; k++) f[k] = (E)(v[k] * down);
-    ((F *)lds)[(r / 16 * NC + d / 32) * 64 + d / 8 % 4 * 16 + r % 16] = f;
+    for (int k = 0; k < 8; k++) {
+      const float y = as_f32(v[k] * down);
+      head[k] = (E)y;
+      tail[k] = (E)(y - (float)head[k]);
+    }
+    F *to = (F *)lds + (r / RT * NC + d / 32) * 64 + d / 8 % 4 * 16 + r % RT;
+    to[0] = head;
+    if (WIDE) to[8] = tail;
   }
   __syncthreads();
-  const int wave_row = rt * ROWS + wave * NQ * 16;
+  const int wave_row = rt * ROWS + wave * NQ * RT, own = col & (RT - 1);
+  const float tails = col < 8 ? 0.f : 1.f;
   F q[NQ][NC];
   float to_log2[NQ];
   int pos[NQ];
 #pragma unroll
   for (int k = 0; k < NQ; k++) {
-    const int row = wave_row + k * 16 + col;
+    const int row = wave_row + k * RT + own;
     pos[k] = row < R ? first + row / G : -1;
     to_log2[k] = lds_scale[row - rt * ROWS];
 #pragma unroll
@@ -94,7 +104,7 @@ __global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_pro
   }
   __syncthreads();
   // positions of the wave's rows
-  const int w_min = wave_row < R ? first + wave_row / G : 0, w_max = wave_row < R ? first + min(wave_row + NQ * 16 - 1, R - 1) / G : -1;
+  const int w_min = wave_row < R ? first + wave_row / G : 0, w_max = wave_row < R ? first + min(wave_row + NQ * RT - 1, R - 1) / G : -1;
   const int w_low = a.window > 0 ? max(w_min - a.window + 1, 0) : 0;
 
   const int sub_bits = c.page_shift - 5;
@@ -228,6 +238,12 @@ __global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_pro
 #pragma unroll
           for (int k = 0; k < NQ; k++) y[k][t] = mma(kf, q[k][e], y[k][t]);
         }
+      if (WIDE) {
+#pragma unroll
+        for (int k = 0; k < NQ; k++)
+#pragma unroll
+          for (int d = 0; d < 8; d++) y[k][d / 4][d % 4] += eight_on(y[k][d / 4][d % 4]);
+      }
       if (!all_seen) {
 #pragma unroll
         for (int k = 0; k < NQ; k++) {
@@ -266,7 +282,10 @@ __global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_pro
           weigh();
         }
 #pragma unroll
-        for (int d = 0; d < 8; d++) p[k][d] = (E)__builtin_amdgcn_exp2f(z[d]);
+        for (int d = 0; d < 8; d++) {
+          const float x = __builtin_amdgcn_exp2f(z[d]);
+          p[k][d] = WIDE ? (E)__builtin_fmaf(-(float)(E)x, tails, x) : (E)x;
+        }
       }
 #pragma unroll
       for (int k = 0; k < NQ; k++) sum[k] = mma(ones, p[k], sum[k]);
@@ -285,8 +304,16 @@ __global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_pro
   const long part0 = ((long)((i * a.row_tiles + rt) * c.heads + h) * a.splits + split) * a.part_rows;
 #pragma unroll
   for (int k = 0; k < NQ; k++) {
-    const int row = wave_row + k * 16 + col;
-    const float l = sum[k][0];
+    const int row = wave_row + k * RT + own;
+    float l = sum[k][0];
+    if (WIDE) {
+      l += eight_on(l);
+#pragma unroll
+      for (int n = 0; n < NV; n++)
+#pragma unroll
+        for (int d = 0; d < 4; d++) o[k][n][d] = head_and_tail(o[k][n][d]);
+      if (col >= 8) continue;
+    }
     if (row >= R) continue;
     if (w.shares > 1) {
       const long r = part0 + row - rt * ROWS;
@@ -319,7 +346,7 @@ __global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_pro
     else if (a.out_type == IO_F16) rows((_Float16 *)a.out);
     else rows((__bf16 *)a.out);
   }
-  if (!lds_strange) return;
+  if (!lds_strange || (WIDE && col >= 8)) return;
   // The infinities and NaN that were left out reach the rows that see them: a lane corrects what it has stored.
   for (int t = t0; t < t1; t++) {
     const int pg = page_of(t), j0 = tile_of(t) * kTile;
@@ -337,7 +364,7 @@ __global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_pro
           if (v - v == 0.f) continue;
         }
         for (int k = 0; k < NQ; k++) {
-          const int row = wave_row + k * 16 + col, p = row < R ? first + row / G : -1;
+          const int row = wave_row + k * RT + own, p = row < R ? first + row / G : -1;
           if (j0 + key > p || (a.window > 0 && j0 + key < p - a.window + 1 && j0 + key >= a.sinks)) continue;
           if (w.shares > 1) {
             a.part[(part0 + row - rt * ROWS) * DH + dim] += v;
@@ -352,34 +379,39 @@ __global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_pro
 
 template <int KIND, int DH>
 struct PromptLaunch {
-  static constexpr int kRows = PromptShape<KIND, DH>::NW * PromptShape<KIND, DH>::NQ * 16, kTiles = 2 * 128 * DH, kQueries = kRows * DH * 2;
+  static constexpr int kColumns = PromptShape<KIND, DH>::NW * PromptShape<KIND, DH>::NQ * 16, kTiles = 2 * 128 * DH, kQueries = kColumns * DH * 2;
   static constexpr int kLds = kTiles > kQueries ? kTiles : kQueries;  // first the queries, then the tiles
 };
 
 template <int KIND, int DH>
 hipError_t launch(CacheAttnArgs a, long tiles, hipStream_t s) {
-  constexpr int kRows = PromptLaunch<KIND, DH>::kRows;
-  a.row_tiles = (int)(((long)a.r.max_new * a.group + kRows - 1) / kRows);
+  const bool wide = a.type == IO_F32;
+  const int rows = PromptLaunch<KIND, DH>::kColumns / (wide ? 2 : 1);
+  a.row_tiles = (int)(((long)a.r.max_new * a.group + rows - 1) / rows);
   const long units = (long)a.r.n * a.c.heads, groups = units * a.row_tiles;
   // Shares of the keys where there are fewer workgroups than the chip holds, two to a CU, of kTurns tiles at least.
   constexpr int kTurns = 8;
-  a.tile_rows = a.part_rows = kRows;
-  const long slots = a.part_floats / (kRows * (DH + 2));
+  a.tile_rows = a.part_rows = rows;
+  const long slots = a.part_floats / (rows * (DH + 2));
   a.splits = (int)std::max<long>(1, std::min({kFill / groups, tiles / kTurns, slots / groups, (long)kMaxSplits}));
   a.least = kTurns;
-  a.part_sums = (float2 *)(a.part + slots * kRows * DH);
+  a.part_sums = (float2 *)(a.part + slots * rows * DH);
   // spread over the dies by unit where that leaves none idle
   const int spread = units % 8 == 0 || units >= 64;
   const long blocks = (spread ? (units + 7) / 8 * 8 : units) * a.row_tiles * a.splits;
-  hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH>), dim3((unsigned)blocks), dim3(PromptShape<KIND, DH>::NW * 64),
-                     (PromptLaunch<KIND, DH>::kLds), s, a, spread);
+  const dim3 grid((unsigned)blocks), block(PromptShape<KIND, DH>::NW * 64);
+  if (wide) hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, true>), grid, block, (PromptLaunch<KIND, DH>::kLds), s, a, spread);
+  else hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, false>), grid, block, (PromptLaunch<KIND, DH>::kLds), s, a, spread);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || a.splits == 1 ? e : launch_cache_join(a, s);
 }
 
 template <int KIND, int DH>
 hipError_t prepare() {
-  return hipFuncSetAttribute((const void *)cache_prompt_kernel<KIND, DH>, hipFuncAttributeMaxDynamicSharedMemorySize, PromptLaunch<KIND, DH>::kLds);
+  const hipError_t e = hipFuncSetAttribute((const void *)cache_prompt_kernel<KIND, DH, false>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           PromptLaunch<KIND, DH>::kLds);
+  return e != hipSuccess ? e : hipFuncSetAttribute((const void *)cache_prompt_kernel<KIND, DH, true>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                   PromptLaunch<KIND, DH>::kLds);
 }
 template <int KIND>
 hipError_t prepare_width(int dh) {

@@ -187,6 +187,31 @@ def test_tokens_over_many_keys(torch, nt, kind, io, lens, max_keys):
     f.cache.check()
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("heads,width", [((4, 2), 64), ((6, 2), 128), ((2, 2), 256), ((1, 1), 512)])
+def test_prompts_of_fp32_keep_twice_the_bits(torch, nt, kind, heads, width):
+    """Within the tolerance of single tokens, also where the keys are shared by workgroups and where infinities are among the values."""
+    past, new = [0, 33, 2500], [150, 70, 41]
+    f = Filled(torch, nt, kind, "f32", past, heads, width, 64, seed=width, spare=12)
+    first, r = ints(torch, rows_of(new)), rows_of(new)
+    f.cache.reserve(3, first=first)
+    k, v, q = f.random(sum(new), heads[1]), f.random(sum(new), heads[1]), f.random(sum(new), heads[0])
+    hk, hv = held(torch, kind, k), held(torch, kind, v)
+    for i in range(3):
+        f.k[0][i], f.v[0][i] = np.concatenate([f.k[0][i], hk[r[i]:r[i + 1]]]), np.concatenate([f.v[0][i], hv[r[i]:r[i + 1]]])
+    for window, sinks in [(0, 0), (100, 3)]:
+        out = torch.empty_like(q)
+        f.cache.attend(q, out, 3, first=first, k=k, v=v, max_new=150, window=window, sinks=sinks)
+        want, tol = f.expect(q, new, range(3), window, sinks, tokens=True)
+        compare(out, want, tol)
+    if kind != "q4":
+        again, v[100] = torch.empty_like(out), float("-inf")
+        f.cache.attend(q, again, 3, first=first, k=k, v=v, max_new=150, window=100, sinks=3)
+        assert torch.equal(again[:100], out[:100]) and torch.equal(again[150:], out[150:])
+        assert (again[100:150] == float("-inf")).all()
+    f.cache.check()
+
+
 @pytest.mark.parametrize("kind,io", [("bf16", "f32"), ("f16", "bf16"), ("bf16", "f16")])
 def test_other_pairs_of_types(torch, nt, kind, io):
     f = Filled(torch, nt, kind, io, [1, 40, 300], (4, 2), 128, 64, seed=2)
