@@ -43,6 +43,9 @@ __global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_pro
   typedef typename FragType<KIND>::elem E;
   constexpr int NQ = PromptShape<KIND, DH>::NQ, NW = PromptShape<KIND, DH>::NW;
   constexpr int NC = DH / 32, NV = DH / 16, TB = 128 * DH, RT = WIDE ? 8 : 16, ROWS = NW * NQ * RT;
+  // Fragments are read from the LDS two ahead of their products, the first values' before the softmax: 128 / 512 wide 934 -> 951 / 704 ->
+  // 786 TFLOP/s.  Not where the registers are full (256 wide, 4 bits: 717 -> 304) or waves are many (64 wide, 4 bits: 626 -> 561).
+  constexpr bool SOON = !(KIND == CACHE_Q4 && (DH == 64 || DH == 256));
   extern __shared__ __align__(1024) char lds[];  // [2][TB], before that the queries
   const CacheView &c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g4 = lane >> 4, G = a.group;
@@ -230,14 +233,17 @@ __global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_pro
       f32x4 y[NQ][2];
 #pragma unroll
       for (int k = 0; k < NQ; k++) y[k][0] = y[k][1] = zero;
+      F kf[2];
+      if (SOON) kf[0] = keys[0], kf[1] = keys[64];
 #pragma unroll
-      for (int t = 0; t < 2; t++)
+      for (int e = 0; e < 2 * NC; e++) {
+        const F now = SOON ? kf[e & 1] : keys[e * 64];
+        if (SOON && e + 2 < 2 * NC) kf[e & 1] = keys[(e + 2) * 64];
 #pragma unroll
-        for (int e = 0; e < NC; e++) {
-          const F kf = keys[(t * NC + e) * 64];
-#pragma unroll
-          for (int k = 0; k < NQ; k++) y[k][t] = mma(kf, q[k][e], y[k][t]);
-        }
+        for (int k = 0; k < NQ; k++) y[k][e / NC] = mma(now, q[k][e % NC], y[k][e / NC]);
+      }
+      F vf[2];
+      if (SOON) vf[0] = values[0], vf[1] = values[64];
       if (WIDE) {
 #pragma unroll
         for (int k = 0; k < NQ; k++)
@@ -291,9 +297,10 @@ __global__ __launch_bounds__((PromptShape<KIND, DH>::NW * 64), 2) void cache_pro
       for (int k = 0; k < NQ; k++) sum[k] = mma(ones, p[k], sum[k]);
 #pragma unroll
       for (int n = 0; n < NV; n++) {
-        const F vf = values[n * 64];
+        const F now = SOON ? vf[n & 1] : values[n * 64];
+        if (SOON && n + 2 < NV) vf[n & 1] = values[(n + 2) * 64];
 #pragma unroll
-        for (int k = 0; k < NQ; k++) o[k][n] = mma(vf, p[k], o[k][n]);
+        for (int k = 0; k < NQ; k++) o[k][n] = mma(now, p[k], o[k][n]);
       }
     }
     place(next, buf ^ 1);
