@@ -351,8 +351,8 @@ int nt_cache_write(nt_cache *c, int32_t layer, int32_t n, const int32_t *d_seq, 
  * seen.  out = sum_j w_j v_j / sum_j w_j with w_j = exp(scale * q . k_j) over the seen keys, zeros where none is seen.
  *   q, out     [rows, n_q_heads, d_head] of `type`, ld_q / ld_out elements from row to row
  *   k, v       NULL, or the rows' keys and values, which are written to the cache first as by nt_cache_write
- *   max_new    no sequence has more query rows (a sequence that has more, or more than its length, gets zeros in the
- *              rows that are too many and is reported)
+ *   max_new    no sequence has more query rows (one that has is reported, and its further rows are left as they were; rows
+ *              before a sequence's first token, where it has more rows than tokens, get zeros and are reported)
  *   max_keys   the longest of the sequences, as far as the caller knows; chooses how the work is split, nothing else.
  *              0 = max_len
  * Keys and values that a query does not see have no influence on it, whatever they are; infinities that it sees give

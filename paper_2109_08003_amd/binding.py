@@ -389,8 +389,11 @@ class Cache:
         # what every call needs, looked up once: a step of a few sequences is a call of a few microseconds
         import torch
         self._lib, self._int32, self._types = lib(), torch.int32, {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
-        self._current_stream, self._scale = torch.cuda.current_stream, d_head ** -0.5
-        self._device = torch.cuda.current_device() if torch.cuda.is_available() else 0
+        self._device = device = torch.cuda.current_device() if torch.cuda.is_available() else 0
+        self._scale = d_head ** -0.5
+        # the current stream's handle without an object around it, where torch offers that: three microseconds less
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._current_stream = (lambda: raw(device)) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
         self._args = NtAttendArgs(C.sizeof(NtAttendArgs))
         self._args_ref = C.byref(self._args)
 
@@ -406,7 +409,7 @@ class Cache:
         return int(lib().nt_cache_bytes(C.byref(c)))
 
     def _stream(self, stream) -> int:
-        return (self._current_stream() if stream is None else stream).cuda_stream
+        return self._current_stream() if stream is None else stream.cuda_stream
 
     def close(self):
         if getattr(self, "_h", None):
