@@ -185,6 +185,10 @@ __global__ __launch_bounds__(kPlan) void cache_reserve_kernel(CacheView c, Cache
   }
 }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// 16 bytes that nobody reads soon: 409 -> 358 us for two layers of 48 sequences of up to 4,200 tokens read out
+__device__ __forceinline__ void stream_out(void *p, u32x4 x) { __builtin_nontemporal_store(x, (u32x4 *)p); }
+
 // ---- contents of pages -----------------------------------------------------------------------------------------------
 
 constexpr int kCopyPiece = 16384;  // bytes a workgroup of 256 copies at a time: four loads in flight per thread
@@ -198,9 +202,9 @@ __device__ void copy_pages(const CacheView &c, int layers, const PageWork &w, in
   for (int k = block / each; k < copies; k += blocks / each) {
     const char *src = base + w.from[k] * c.page_bytes;
     char *dst = base + w.to[k] * c.page_bytes;
-    if ((long)(piece + 1) * kCopyPiece <= c.page_bytes) {
-      const uint4 x0 = *(const uint4 *)src, x1 = *(const uint4 *)(src + 4096), x2 = *(const uint4 *)(src + 8192), x3 = *(const uint4 *)(src + 12288);
-      *(uint4 *)dst = x0, *(uint4 *)(dst + 4096) = x1, *(uint4 *)(dst + 8192) = x2, *(uint4 *)(dst + 12288) = x3;
+    if ((long)(piece + 1) * kCopyPiece <= c.page_bytes) {  // streamed: 24 sequences of 2,500 in 4 bits, 4 layers, 136 -> 105 us
+      const u32x4 x0 = *(const u32x4 *)src, x1 = *(const u32x4 *)(src + 4096), x2 = *(const u32x4 *)(src + 8192), x3 = *(const u32x4 *)(src + 12288);
+      stream_out(dst, x0), stream_out(dst + 4096, x1), stream_out(dst + 8192, x2), stream_out(dst + 12288, x3);
     } else {
       for (int j = 0; at + j < c.page_bytes; j += 4096) *(uint4 *)(dst + j) = *(const uint4 *)(src + j);
     }
@@ -623,8 +627,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadArgs a) {
       if (a.type == IO_F32) {
         float *to = (float *)dst + o;
         if (a.vec) {
-          *(float4 *)to = make_float4(val[0], val[1], val[2], val[3]);
-          *(float4 *)(to + 4) = make_float4(val[4], val[5], val[6], val[7]);
+          stream_out(to, (u32x4{__float_as_uint(val[0]), __float_as_uint(val[1]), __float_as_uint(val[2]), __float_as_uint(val[3])}));
+          stream_out(to + 4, (u32x4{__float_as_uint(val[4]), __float_as_uint(val[5]), __float_as_uint(val[6]), __float_as_uint(val[7])}));
         } else {
 #pragma unroll
           for (int j = 0; j < 8; j++) to[j] = val[j];
@@ -636,7 +640,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadArgs a) {
           w[j] = a.type == IO_F16 ? __builtin_bit_cast(unsigned short, (_Float16)val[j]) : __builtin_bit_cast(unsigned short, (__bf16)val[j]);
         unsigned short *to = (unsigned short *)dst + o;
         if (a.vec) {
-          *(uint4 *)to = make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16);
+          stream_out(to, (u32x4{w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16}));
         } else {
 #pragma unroll
           for (int j = 0; j < 8; j++) to[j] = w[j];
