@@ -186,10 +186,6 @@ __device__ __forceinline__ int q4_round(const float (&x)[8], uint32_t &codes) {
   for (int j = 0; j < 8; j++) codes |= (uint32_t)q4_code(x[j], s) << (4 * j);
   return b;
 }
-__device__ __forceinline__ float q4_magnitude(int c) {  // 0, .5, 1, 1.5, 2, 3, 4, 6
-  const int e = (c >> 1) & 3, m = c & 1;
-  return e == 0 ? 0.5f * m : (float)((2 + m) << e) * 0.25f;
-}
 #endif
 
 }  // namespace nt

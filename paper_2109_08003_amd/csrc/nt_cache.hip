@@ -12,7 +12,7 @@
 #include <new>
 
 #include "../../include/nt.h"
-#include "nt_cache.h"
+#include "nt_cache_frag.h"
 #include "nt_cache_host.h"
 #include "nt_kernels.h"
 
@@ -607,13 +607,17 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadArgs a) {
         if constexpr (KIND == CACHE_Q4) {
           const unsigned char *scales = (const unsigned char *)at + 32 * dh;
           const float sc = q4_scale(side == 0 ? scales[tok * (dh / 32) + (dim >> 5)] : scales[dh + (dim >> 5) * kTile + tok]);
-          const uint32_t word = side == 0 ? ((const uint32_t *)at)[q4_key_word(tok, dim, dh)] : 0;
+          uint32_t word = 0;
+          if (side == 0) {
+            word = ((const uint32_t *)at)[q4_key_word(tok, dim, dh)];
+          } else {
 #pragma unroll
-          for (int j = 0; j < 8; j++) {
-            const int code = side == 0 ? (word >> (4 * j)) & 15 : (lds[q4_value_word(tok, own + j)] >> (4 * (tok & 7))) & 15;
-            val[j] = q4_magnitude(code & 7) * sc;
-            if (code & 8) val[j] = -val[j];
+            for (int j = 0; j < 8; j++) word |= (lds[q4_value_word(tok, own + j)] >> (4 * (tok & 7)) & 15u) << (4 * j);
           }
+          f16x2 h[4];
+          q4_unpack(word, h);
+#pragma unroll
+          for (int j = 0; j < 8; j++) val[j] = (float)h[j / 2][j % 2] * sc;
         } else {
 #pragma unroll
           for (int j = 0; j < 8; j++) {
