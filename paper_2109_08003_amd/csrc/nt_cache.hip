@@ -77,9 +77,9 @@ __device__ int count_free(const CacheView &c, int32_t (&lds)[kPlan / 64]) {
   for (int w = threadIdx.x; w < words_of(c); w += kPlan) n += __popc(~c.used[w]);
   return block_sum(n, lds);
 }
-// list[0 .. n) = the lowest n free pages, now held once
+// list[0 .. n) = the lowest n free pages, of which there are that many, now held once
 __device__ void take_pages(const CacheView &c, int n, int32_t *list, int32_t (&lds)[kPlan / 64]) {
-  for (int w0 = 0, done = 0; done < n; w0 += kPlan) {  // there are n free pages
+  for (int w0 = 0, done = 0; done < n && w0 < words_of(c); w0 += kPlan) {
     const int w = w0 + threadIdx.x;
     uint32_t free = w < words_of(c) ? ~c.used[w] : 0, got = 0;
     int all, at = done + block_scan(__popc(free), all, lds);
@@ -488,10 +488,10 @@ __global__ __launch_bounds__(kPlan) void cache_lengths_kernel(CacheView c, int32
   }
 }
 
-__global__ __launch_bounds__(256) void cache_clear_kernel(CacheView c) {
+__global__ __launch_bounds__(256) void cache_clear_kernel(CacheView c, PageWork w) {
   const long i = (long)blockIdx.x * 256 + threadIdx.x, words = (c.n_pages + 31) / 32;
   if (i < c.max_seqs) c.len[i] = c.base[i] = 0, c.slot[i] = -1, c.mark[i] = INT_MAX;
-  if (i < c.n_pages) c.ref[i] = 0;
+  if (i < c.n_pages) c.ref[i] = w.list[i] = 0;
   if (i < words) c.used[i] = i * 32 + 32 <= c.n_pages ? 0 : ~((1u << (c.n_pages & 31)) - 1);  // bits behind the last page: never free
   if (i < 2) c.flags[i] = 0;
 }
@@ -784,7 +784,7 @@ int become(nt_cache *c, int32_t n, const int32_t *d_src, const int32_t *d_dst, i
   if (!d_src || !d_dst) return fail(NT_EINVAL, "null argument");
   hipStream_t s = as_stream(hip_stream);
   // A table of few rows is the planning workgroup's as well: one launch less to enqueue.  48 entries of one page or two, with the
-  // reading of what they became: 19 us of the host's time and 22 in all, 23 and 24 with the table's launches of their own.
+  // reading of what they became: 4 us less of the host's time and 2 less in all (of 24) than with a launch of the table's own.
   const int whole = (double)n * c->v.width > 4096 ? 0 : c->v.width <= 16 ? 16 : 64, tables = whole ? 0 : n;
   const int copies = nt::copy_blocks(c->v, c->cfg.n_layers, deep ? (double)n * c->v.width : n);
   hipLaunchKernelGGL(nt::cache_fork_plan_kernel, dim3(1), dim3(nt::kPlan), 0, s, c->v, n, d_src, d_dst, deep, whole, c->w);
@@ -827,7 +827,7 @@ int nt_cache_create(const nt_cache_config *cfg, void *hip_stream, nt_cache **out
     lay_out(c, c->mem);
     HIP_TRY(nt::prepare_cache_prompt(cfg->kind, cfg->d_head));
     const int most = std::max(cfg->n_pages, cfg->max_seqs);
-    hipLaunchKernelGGL(nt::cache_clear_kernel, dim3((most + 255) / 256), dim3(256), 0, as_stream(hip_stream), c->v);
+    hipLaunchKernelGGL(nt::cache_clear_kernel, dim3((most + 255) / 256), dim3(256), 0, as_stream(hip_stream), c->v, c->w);
     HIP_TRY(hipGetLastError());
     HIP_TRY(hipStreamSynchronize(as_stream(hip_stream)));
     return NT_OK;
